@@ -411,6 +411,125 @@ cci_status cci_global_avgpool_nhwc(const void *X, cci_dtype x_t, int64_t B,
                                    int64_t H, int64_t W, int64_t C, void *Y,
                                    cci_dtype y_t, void *stream);
 
+/* ------------------------------------------------------------------------
+ * A transformer's feed-forward block of CCI layers (not from the paper):
+ * layer norm, the gated product of two CCI projections, the input gradient
+ * of a CCI product for any G and K, and low-rank adapters beside a shared
+ * CCI projection.  Each computes one type t throughout (F32 or BF16, weights
+ * included) with fp32 sums; any sizes; rows need no alignment of their own.
+ * ------------------------------------------------------------------------ */
+
+/* Layer norm of each row of X [N][C]:
+ *   m = mean(x), s = 1 / sqrt(mean((x - m)^2) + eps),
+ *   Y[n][c] = (x - m) * s * gamma[c] + beta[c].
+ * gamma, beta: fp32 [C] or NULL (1, 0).  Y: [N][C] of t.  mean, rstd: fp32
+ * [N] outputs (m and s), or NULL; the backward pass reads them.  eps >= 0
+ * (with eps = 0 a row of equal values is 0 / 0). */
+cci_status cci_layernorm(const void *X, cci_dtype t, int64_t N, int64_t C,
+                         const float *gamma, const float *beta, float eps,
+                         void *Y, float *mean, float *rstd, void *stream);
+
+/* Bytes of the workspace of cci_layernorm_bwd: the partial sums of the weight
+ * gradients (at most 256 x 2 x C fp32, more for C > 16384). */
+cci_status cci_layernorm_bwd_workspace(int64_t N, int64_t C, size_t *bytes);
+
+/* Its backward pass: with xh = (x - mean) * rstd and q = dY * gamma,
+ *   dX = rstd * (q - mean_c(q) - xh * mean_c(q * xh)),
+ *   dgamma[c] = sum_n dY * xh,   dbeta[c] = sum_n dY.
+ * dX [N][C] of t, dgamma and dbeta fp32 [C]; each may be NULL.  N == 0
+ * writes zeros to dgamma and dbeta.  The sums run in a fixed order: equal
+ * calls give equal bits.  workspace: device memory that nothing else uses
+ * until the call's work is done. */
+cci_status cci_layernorm_bwd(const void *dY, const void *X, cci_dtype t,
+                             int64_t N, int64_t C, const float *gamma,
+                             const float *mean, const float *rstd, void *dX,
+                             float *dgamma, float *dbeta, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
+/* The activation of a gated product: x, max(x, 0), x / (1 + exp(-x)),
+ * x * Phi(x), and the tanh approximation of the last. */
+typedef enum {
+  CCI_ACT_NONE = 0,
+  CCI_ACT_RELU = 1,
+  CCI_ACT_SILU = 2,
+  CCI_ACT_GELU = 3,
+  CCI_ACT_GELU_TANH = 4
+} cci_act;
+
+/* Gated product of two CCI projections in one kernel:
+ *   P = X . W_hat^T,   H[n][f] = act(P[n][f]) * P[n][F + f].
+ * vals / idx: one packing, as from cci_pack, of the stacked [2F][C] matrix
+ * (gate rows, then up rows), F % G == 0, vals of t.  H: [N][F] of t.  pre:
+ * [N][2F] of t, the preactivations P (rounded) for the backward pass, or
+ * NULL.  H is computed from the unrounded P.  An infinity or NaN in X[n][c]
+ * may make every output of row n NaN; other rows see none of it. */
+cci_status cci_gated_spmm(const void *X, cci_dtype t, int64_t N, int64_t C,
+                          const void *vals, const uint8_t *idx, int64_t F,
+                          int32_t G, int32_t K, cci_act act, void *H,
+                          void *pre, void *stream);
+
+/* Its backward pass from the saved preactivations (g, u) = pre:
+ *   dpre[n] = (dH * u * act'(g), dH * act(g)),
+ *   dX = dpre . W_hat,
+ *   dvals[g][k][c] = sum_n dpre[n][gG + idx[g][k][c]] * X[n][c].
+ * dH: [N][F], pre: [N][2F], X: [N][C], all of t.  dpre: [N][2F] of t, an
+ * output that the two products read (with t = BF16 they take its rounded
+ * values).  dX: [N][C] of t, or NULL.  dvals: [2F/G][K][C] of dv_t (F32, or
+ * BF16 with t = BF16), or NULL.  act'(0) of the ReLU is 0.  N == 0 writes
+ * zeros to dvals.  vals may be NULL without dX, X without dvals. */
+cci_status cci_gated_spmm_bwd(const void *dH, const void *pre, const void *X,
+                              cci_dtype t, int64_t N, int64_t C,
+                              const void *vals, const uint8_t *idx, int64_t F,
+                              int32_t G, int32_t K, cci_act act, void *dpre,
+                              void *dX, void *dvals, cci_dtype dv_t,
+                              void *stream);
+
+/* Input gradient of a CCI product, dX = dY . W_hat, from the packing itself
+ * for any G and K (cci_to_2of4_transposed + cci_spmm_2of4 take K <= 2):
+ *   dX[n][c] = sum_g sum_k vals[g][k][c] * dY[n][gG + idx[g][k][c]].
+ * dY: [N][O] of t; vals / idx as from cci_pack, vals of t; dX: [N][C] of
+ * dx_t (F32, or BF16 with t = BF16).  An infinity or NaN in dY[n] may make
+ * the whole row of dX NaN. */
+cci_status cci_spmm_t(const void *dY, cci_dtype t, int64_t N, int64_t O,
+                      const void *vals, const uint8_t *idx, int64_t C,
+                      int32_t G, int32_t K, void *dX, cci_dtype dx_t,
+                      void *stream);
+
+/* Low-rank adapters of many requests.  Row n of a product has the adapter
+ * a = rows[n] (device int32 [N]); outside [0, L) it has none.  A: [L][R][C]
+ * and B: [L][O][R] of X's type, alpha: fp32 [L] or NULL (1).  1 <= R <= 1024;
+ * adapters of a lower rank are padded with zeros. */
+typedef struct {
+  const void *A;
+  const void *B;
+  const float *alpha;
+  const int32_t *rows;
+  int64_t L;
+  int32_t R;
+} cci_adapters;
+
+/* Bytes of the workspace of cci_spmm_adapters (the adapters' term in Y's
+ * type and the partial sums of A . x). */
+cci_status cci_spmm_adapters_workspace(int64_t N, int64_t C, int64_t O,
+                                       int64_t L, int32_t R, cci_dtype y_t,
+                                       size_t *bytes);
+
+/* The product of cci_spmm with a low-rank term per row:
+ *   D[n][o] = residual[n][o] + alpha[a] * sum_r B[a][o][r] (A[a][r] . X[n]),
+ *   Y[n][o] = relu?( acc * scale[o] + bias[o] + D[n][o] ),
+ * acc the CCI product; D is rounded to Y's type before it is added.  Types
+ * as for cci_spmm; G may be any from 1 to 256.  Rows may come in any order;
+ * rows of one request next to each other share its weights' reads.  The sums
+ * run in a fixed order.  Non-finite values as for cci_spmm's bf16 families;
+ * those of one adapter reach its rows alone. */
+cci_status cci_spmm_adapters(const void *X, cci_dtype x_t, int64_t N,
+                             int64_t C, const void *vals, cci_dtype val_t,
+                             const uint8_t *idx, int64_t O, int32_t G,
+                             int32_t K, const cci_adapters *adapters,
+                             const cci_epilogue *ep, void *Y, cci_dtype y_t,
+                             void *workspace, size_t workspace_bytes,
+                             void *stream);
+
 /* Static description of a status code. */
 const char *cci_status_str(cci_status s);
 

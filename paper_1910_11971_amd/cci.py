@@ -28,6 +28,9 @@ ALGOS = {"auto": ALGO_AUTO, "sparse_mac": ALGO_SPARSE_MAC, "dense_tile_mfma": AL
          "split_k_mfma": ALGO_SPLIT_K_MFMA}
 
 
+ACTS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+
+
 class CCIError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"status {status}: {msg}")
@@ -37,6 +40,11 @@ class CCIError(RuntimeError):
 class Epilogue(ctypes.Structure):
     _fields_ = [("scale", ctypes.c_void_p), ("bias", ctypes.c_void_p),
                 ("residual", ctypes.c_void_p), ("relu", ctypes.c_int32)]
+
+
+class Adapters(ctypes.Structure):
+    _fields_ = [("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("alpha", ctypes.c_void_p),
+                ("rows", ctypes.c_void_p), ("L", ctypes.c_int64), ("R", ctypes.c_int32)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -78,6 +86,16 @@ _lib.cci_last_algo.argtypes = []
 _lib.cci_last_algo.restype = ctypes.c_int
 _lib.cci_maxpool2d_nhwc.argtypes = [_vp, ctypes.c_int, _i64, _i64, _i64, _i64, _i32, _i32, _i32, _vp, _vp]
 _lib.cci_global_avgpool_nhwc.argtypes = [_vp, ctypes.c_int, _i64, _i64, _i64, _i64, _vp, ctypes.c_int, _vp]
+_lib.cci_layernorm.argtypes = [_vp, ctypes.c_int, _i64, _i64, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]
+_lib.cci_layernorm_bwd_workspace.argtypes = [_i64, _i64, ctypes.POINTER(_sz)]
+_lib.cci_layernorm_bwd.argtypes = [_vp, _vp, ctypes.c_int, _i64, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.cci_gated_spmm.argtypes = [_vp, ctypes.c_int, _i64, _i64, _vp, _vp, _i64, _i32, _i32, ctypes.c_int, _vp, _vp, _vp]
+_lib.cci_gated_spmm_bwd.argtypes = [_vp, _vp, _vp, ctypes.c_int, _i64, _i64, _vp, _vp, _i64, _i32, _i32, ctypes.c_int,
+                                    _vp, _vp, _vp, ctypes.c_int, _vp]
+_lib.cci_spmm_t.argtypes = [_vp, ctypes.c_int, _i64, _i64, _vp, _vp, _i64, _i32, _i32, _vp, ctypes.c_int, _vp]
+_lib.cci_spmm_adapters_workspace.argtypes = [_i64, _i64, _i64, _i64, _i32, ctypes.c_int, ctypes.POINTER(_sz)]
+_lib.cci_spmm_adapters.argtypes = [_vp, ctypes.c_int, _i64, _i64, _vp, ctypes.c_int, _vp, _i64, _i32, _i32,
+                                   ctypes.POINTER(Adapters), ctypes.POINTER(Epilogue), _vp, ctypes.c_int, _vp, _sz, _vp]
 _lib.cci_status_str.argtypes = [ctypes.c_int]
 _lib.cci_status_str.restype = ctypes.c_char_p
 _lib.cci_last_error.restype = ctypes.c_char_p
@@ -86,7 +104,8 @@ for _fn in ("cci_packed_sizes", "cci_pack", "cci_spmm", "cci_spmm_algo", "cci_co
             "cci_conv_im2col_algo", "cci_maxpool2d_nhwc", "cci_global_avgpool_nhwc", "cci_bbs_packed_sizes",
             "cci_bbs_pack", "cci_2of4_sizes", "cci_bbs_to_2of4", "cci_to_2of4_transposed", "cci_spmm_2of4",
             "cci_td_schedule", "cci_td_mask", "cci_grad_packed", "cci_index_stream_bytes", "cci_index_bits",
-            "cci_spmm_bits"):
+            "cci_spmm_bits", "cci_layernorm", "cci_layernorm_bwd_workspace", "cci_layernorm_bwd", "cci_gated_spmm",
+            "cci_gated_spmm_bwd", "cci_spmm_t", "cci_spmm_adapters_workspace", "cci_spmm_adapters"):
     getattr(_lib, _fn).restype = ctypes.c_int
 
 
@@ -436,4 +455,180 @@ def spmm_bits(X: torch.Tensor, vals: torch.Tensor, idx: torch.Tensor, G: int, id
     ep = _epilogue(scale, bias, residual, relu, O, Y.shape, Y.dtype, X.device)
     _check(_lib.cci_spmm_bits(_ptr(X), _code(X.dtype), N, C, _ptr(vals), _code(vals.dtype), _ptr(idx), idx_bits, O, G,
                               K, ep, _ptr(Y), _code(Y.dtype), _stream(X)))
+    return Y
+
+
+# ------------------------------------------------------ feed-forward block --
+
+class _on:
+    """The device of a call's tensors made current for its launches (a launch
+    on another device's stream is an error); nothing to do when it is."""
+    __slots__ = ("dev", "back")
+
+    def __init__(self, dev):
+        self.dev, self.back = dev.index, -1
+
+    def __enter__(self):
+        if self.dev is not None and self.dev != torch.cuda.current_device():
+            self.back = torch.cuda.current_device()
+            torch.cuda.set_device(self.dev)
+
+    def __exit__(self, *exc):
+        if self.back >= 0:
+            torch.cuda.set_device(self.back)
+
+
+def _tensor(t, name, shape, dtype, device):
+    """Check a contiguous input tensor of one shape, dtype and device."""
+    _dev(t)
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+    return t
+
+
+def _packed(vals, idx, G, O, C, dtype, device):
+    """Check packed weights of an [O, C] matrix (O None: any); K and O."""
+    _dev(vals), _dev(idx)
+    if vals.dim() != 3 or idx.shape != vals.shape or idx.dtype != torch.uint8 or vals.dtype != dtype:
+        raise ValueError(f"packed weights must be (vals, idx) of one shape [O/G, K, C], {dtype} and uint8")
+    if vals.device != device or idx.device != device:
+        raise ValueError("the packed weights must be on the input's device")
+    ng, K, C2 = vals.shape
+    if (C is not None and C2 != C) or (O is not None and ng * G != O):
+        raise ValueError(f"packed weights of shape {tuple(vals.shape)} do not match G={G}, O={O}, C={C}")
+    return K, ng * G
+
+
+def _matrix(X, name):
+    _dev(X)
+    if X.dim() != 2:
+        raise ValueError(f"{name} must be a matrix")
+    return X.shape
+
+
+def layernorm(X: torch.Tensor, gamma=None, beta=None, eps: float = 1e-5, *, out=None):
+    """cci_layernorm over the rows of X [N, C]: (Y [N, C] of X's dtype, mean
+    fp32 [N], reciprocal standard deviation fp32 [N])."""
+    N, C = _matrix(X, "X")
+    dev = X.device
+    for name, v in (("gamma", gamma), ("beta", beta)):
+        if v is not None:
+            _tensor(v, name, (C,), torch.float32, dev)
+    code = _code(X.dtype)
+    Y = _out(out, (N, C), X.dtype, dev)
+    mean, rstd = torch.empty(N, dtype=torch.float32, device=dev), torch.empty(N, dtype=torch.float32, device=dev)
+    with _on(dev):
+        _check(_lib.cci_layernorm(_ptr(X), code, N, C, _ptr(gamma), _ptr(beta), eps, _ptr(Y), _ptr(mean), _ptr(rstd),
+                                  _stream(X)))
+    return Y, mean, rstd
+
+
+def layernorm_bwd(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, gamma=None, *,
+                  need_dx=True, need_dw=True):
+    """cci_layernorm_bwd: (dX [N, C] of X's dtype, dgamma fp32 [C], dbeta fp32
+    [C]); those not needed are None.  The workspace comes from torch's
+    allocator on the current stream."""
+    N, C = _matrix(X, "X")
+    dev = X.device
+    _tensor(dY, "dY", (N, C), X.dtype, dev)
+    _tensor(mean, "mean", (N,), torch.float32, dev), _tensor(rstd, "rstd", (N,), torch.float32, dev)
+    if gamma is not None:
+        _tensor(gamma, "gamma", (C,), torch.float32, dev)
+    code = _code(X.dtype)
+    nb = _sz()
+    _check(_lib.cci_layernorm_bwd_workspace(N, C, ctypes.byref(nb)))
+    ws = torch.empty(nb.value, dtype=torch.uint8, device=dev)
+    dX = torch.empty((N, C), dtype=X.dtype, device=dev) if need_dx else None
+    dg, db = (torch.empty(C, dtype=torch.float32, device=dev) if need_dw else None for _ in range(2))
+    with _on(dev):
+        _check(_lib.cci_layernorm_bwd(_ptr(dY), _ptr(X), code, N, C, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dX),
+                                      _ptr(dg), _ptr(db), _ptr(ws), nb.value, _stream(X)))
+    return dX, dg, db
+
+
+def gated_spmm(X: torch.Tensor, vals: torch.Tensor, idx: torch.Tensor, G: int, *, act="silu", save_pre=False,
+               out=None):
+    """cci_gated_spmm: H [N, F] = act(X . Wg^T) * (X . Wu^T) from one packing
+    [2F/G, K, C] of the stacked gate and up weights; with save_pre (H, pre),
+    pre [N, 2F] the preactivations for gated_spmm_bwd."""
+    N, C = _matrix(X, "X")
+    dev = X.device
+    K, O = _packed(vals, idx, G, None, C, X.dtype, dev)
+    if O % 2 or (O // 2) % G:
+        raise ValueError("the packing must hold 2 F rows with F a multiple of G")
+    F = O // 2
+    code = _code(X.dtype)
+    H = _out(out, (N, F), X.dtype, dev)
+    pre = torch.empty((N, O), dtype=X.dtype, device=dev) if save_pre else None
+    with _on(dev):
+        _check(_lib.cci_gated_spmm(_ptr(X), code, N, C, _ptr(vals), _ptr(idx), F, G, K, ACTS[act], _ptr(H), _ptr(pre),
+                                   _stream(X)))
+    return (H, pre) if save_pre else H
+
+
+def gated_spmm_bwd(dH: torch.Tensor, pre: torch.Tensor, X: torch.Tensor, vals: torch.Tensor, idx: torch.Tensor,
+                   G: int, *, act="silu", dvals_dtype=None, need_dx=True, need_dvals=True):
+    """cci_gated_spmm_bwd: (dpre [N, 2F], dX [N, C], dvals [2F/G, K, C]) from
+    the preactivations that gated_spmm saved; dvals of X's dtype unless
+    dvals_dtype says fp32; those not needed are None."""
+    N, C = _matrix(X, "X")
+    dev = X.device
+    K, O = _packed(vals, idx, G, None, C, X.dtype, dev)
+    if O % 2 or (O // 2) % G:
+        raise ValueError("the packing must hold 2 F rows with F a multiple of G")
+    F = O // 2
+    _tensor(dH, "dH", (N, F), X.dtype, dev), _tensor(pre, "pre", (N, O), X.dtype, dev)
+    dv_t = dvals_dtype or X.dtype
+    code, dv_code = _code(X.dtype), _code(dv_t)
+    dpre = torch.empty((N, O), dtype=X.dtype, device=dev)
+    dX = torch.empty((N, C), dtype=X.dtype, device=dev) if need_dx else None
+    dv = torch.empty(vals.shape, dtype=dv_t, device=dev) if need_dvals else None
+    with _on(dev):
+        _check(_lib.cci_gated_spmm_bwd(_ptr(dH), _ptr(pre), _ptr(X), code, N, C, _ptr(vals), _ptr(idx), F, G, K,
+                                       ACTS[act], _ptr(dpre), _ptr(dX), _ptr(dv), dv_code, _stream(X)))
+    return dpre, dX, dv
+
+
+def spmm_t(dY: torch.Tensor, vals: torch.Tensor, idx: torch.Tensor, G: int, *, out_dtype=None, out=None):
+    """cci_spmm_t: dX [N, C] = dY [N, O] . W_hat from the packing, any G and K."""
+    N, O = _matrix(dY, "dY")
+    dev = dY.device
+    K, _ = _packed(vals, idx, G, O, None, dY.dtype, dev)
+    C = vals.shape[2]
+    code = _code(dY.dtype)
+    dX = _out(out, (N, C), out_dtype or dY.dtype, dev)
+    with _on(dev):
+        _check(_lib.cci_spmm_t(_ptr(dY), code, N, O, _ptr(vals), _ptr(idx), C, G, K, _ptr(dX), _code(dX.dtype),
+                               _stream(dY)))
+    return dX
+
+
+def spmm_adapters(X: torch.Tensor, vals: torch.Tensor, idx: torch.Tensor, G: int, A: torch.Tensor, B: torch.Tensor,
+                  rows: torch.Tensor, *, alpha=None, scale=None, bias=None, residual=None, relu=False, out_dtype=None,
+                  out=None) -> torch.Tensor:
+    """cci_spmm_adapters: the product of spmm plus alpha[a] (X A[a]^T) B[a]^T
+    in each row n, a = rows[n] (int32; outside [0, L): no adapter).  A [L, R,
+    C], B [L, O, R] of X's dtype, alpha fp32 [L].  The workspace comes from
+    torch's allocator on the current stream."""
+    N, C = _matrix(X, "X")
+    dev = X.device
+    K, O = _packed(vals, idx, G, None, C, X.dtype, dev)
+    if A.dim() != 3:
+        raise ValueError("A must be [L, R, C]")
+    L, R = A.shape[0], A.shape[1]
+    _tensor(A, "A", (L, R, C), X.dtype, dev), _tensor(B, "B", (L, O, R), X.dtype, dev)
+    _tensor(rows, "rows", (N,), torch.int32, dev)
+    if alpha is not None:
+        _tensor(alpha, "alpha", (L,), torch.float32, dev)
+    code = _code(X.dtype)
+    Y = _out(out, (N, O), out_dtype or X.dtype, dev)
+    ycode = _code(Y.dtype)
+    ep = _epilogue(scale, bias, residual, relu, O, Y.shape, Y.dtype, dev)
+    nb = _sz()
+    _check(_lib.cci_spmm_adapters_workspace(N, C, O, L, R, ycode, ctypes.byref(nb)))
+    ws = torch.empty(nb.value, dtype=torch.uint8, device=dev)
+    ad = Adapters(_ptr(A), _ptr(B), _ptr(alpha), _ptr(rows), L, R)
+    with _on(dev):
+        _check(_lib.cci_spmm_adapters(_ptr(X), code, N, C, _ptr(vals), code, _ptr(idx), O, G, K, ctypes.byref(ad), ep,
+                                      _ptr(Y), ycode, _ptr(ws), nb.value, _stream(X)))
     return Y

@@ -9,12 +9,14 @@
 #include <cstring>
 
 #include "../../include/cci.h"
+#include "cci_check.hpp"
 #include "cci_launch.hpp"
 
+namespace cci {
 namespace {
 
 thread_local char g_last_error[512] = "";
-thread_local cci_algo g_last_algo = CCI_ALGO_AUTO;
+}  // namespace
 
 cci_status fail(cci_status s, const char* fmt, ...) {
   va_list ap;
@@ -29,7 +31,13 @@ cci_status ok() {
   return CCI_OK;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+}  // namespace cci
+
+using namespace cci;
+
+namespace {
+
+thread_local cci_algo g_last_algo = CCI_ALGO_AUTO;
 
 // B * H * W * C < lim, checked without overflow (B >= 0; H, W, C >= 1).
 bool fits_nhwc(int64_t B, int64_t H, int64_t W, int64_t C, int64_t lim) {
@@ -37,24 +45,6 @@ bool fits_nhwc(int64_t B, int64_t H, int64_t W, int64_t C, int64_t lim) {
   const int64_t hw = H * W;
   if (C > lim / hw) return false;            // H * W * C <= lim
   return B <= (lim - 1) / (hw * C);          // B * H * W * C <= lim - 1
-}
-
-bool dtype_ok(cci_dtype t) { return t == CCI_F32 || t == CCI_BF16; }
-
-cci::DType to_dt(cci_dtype t) { return t == CCI_F32 ? cci::DType::F32 : cci::DType::BF16; }
-
-size_t dsize(cci_dtype t) { return t == CCI_F32 ? 4 : 2; }
-
-cci_status check_groups(int64_t O, int64_t C, int32_t G, int32_t K) {
-  if (G < 1 || G > 256) return fail(CCI_EINVAL, "G=%d outside [1, 256]", G);
-  if (K < 1 || K > G) return fail(CCI_EINVAL, "K=%d outside [1, G=%d]", K, G);
-  if (O < 1 || O % G != 0) return fail(CCI_EINVAL, "O=%lld is not a positive multiple of G=%d", (long long)O, G);
-  if (C < 1) return fail(CCI_EINVAL, "C=%lld < 1", (long long)C);
-  // packed arrays and grids are indexed with 64-bit offsets; keep element
-  // counts well inside what the launch grids can cover
-  if (O > (int64_t(1) << 31) || C > (int64_t(1) << 31) || O * C > (int64_t(1) << 40))
-    return fail(CCI_EINVAL, "O*C too large");
-  return CCI_OK;
 }
 
 cci_status check_types(cci_dtype x_t, cci_dtype val_t, cci_dtype y_t) {

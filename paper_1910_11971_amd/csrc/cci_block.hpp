@@ -1,0 +1,69 @@
+// Host-side launcher interface of the feed-forward block's operators (layer
+// norm, gated product, transposed product, adapters) between their C ABI
+// layer (cci_block_api.cpp) and the kernel translation units.  Every launcher
+// assumes validated arguments and returns the HIP status of its launch.
+#pragma once
+
+#include "cci_launch.hpp"
+
+namespace cci {
+
+// Activations (the values of cci_act).
+enum class Act { NONE = 0, RELU = 1, SILU = 2, GELU = 3, GELU_TANH = 4 };
+
+// Layer norm over the last dimension.
+hipError_t launch_layernorm(const void* X, DType t, int64_t N, int64_t C, const float* gamma, const float* beta,
+                            float eps, void* Y, float* mean, float* rstd, hipStream_t s);
+int64_t layernorm_bwd_workspace(int64_t N, int64_t C);
+hipError_t launch_layernorm_bwd(const void* dY, const void* X, DType t, int64_t N, int64_t C, const float* gamma,
+                                const float* mean, const float* rstd, void* dX, float* dgamma, float* dbeta,
+                                void* workspace, hipStream_t s);
+
+// Products over one CCI packing on the matrix cores, any sizes, G and K.
+struct BlockProduct {
+  const void* X;       // gated, plain, grad: X [N][C]
+  const void* dY;      // back, grad: dY [N][O]
+  DType t;
+  int64_t N, C;
+  const void* vals;    // [O/G][K][C] of t
+  const uint8_t* idx;
+  int64_t O;           // gated: 2 F
+  int32_t G, K;
+  Act act;             // gated
+  void* Y;             // gated: H [N][O/2]; plain: [N][O]; back: dX [N][C]; grad: dvals [O/G][K][C]
+  void* pre;           // gated: preactivations [N][O], or null
+  DType y_t;           // plain, back, grad: type of Y
+  const float* scale;  // plain: the epilogue of cci_spmm
+  const float* bias;
+  const void* residual;
+  int32_t relu;
+};
+hipError_t launch_tile_gated(const BlockProduct& a, hipStream_t s);
+hipError_t launch_tile_plain(const BlockProduct& a, hipStream_t s);
+hipError_t launch_tile_back(const BlockProduct& a, hipStream_t s);
+hipError_t launch_tile_grad(const BlockProduct& a, hipStream_t s);
+
+// Gradient of the preactivations of H = act(pre[:, :F]) * pre[:, F:].
+hipError_t launch_gate_grad(const void* dH, const void* pre, DType t, int64_t N, int64_t F, Act act, void* dpre,
+                            hipStream_t s);
+
+// Low-rank adapters: D[n][o] = residual[n][o] + alpha[a] sum_r (sum_c A[a][r][c] X[n][c]) B[a][o][r], a = rows[n]
+// (outside [0, L): the residual alone).
+struct AdapterArgs {
+  const void* X;
+  DType t;
+  int64_t N, C, O, L;
+  int32_t R;
+  const void* A;
+  const void* B;
+  const float* alpha;
+  const int32_t* rows;
+  const void* residual;
+  void* D;
+  DType d_t;
+  float* part;  // workspace of adapter_part_bytes()
+};
+int64_t adapter_part_bytes(int64_t N, int64_t C, int64_t L, int32_t R);
+hipError_t launch_adapters(const AdapterArgs& a, hipStream_t s);
+
+}  // namespace cci

@@ -1,0 +1,76 @@
+// Operand fragments of the 16 x 16 matrix-core products, loads of rows of any
+// alignment and length, and four-element stores, for bf16 and fp32 operands.
+#pragma once
+
+#include <type_traits>
+
+#include "cci_device.hpp"
+
+namespace cci {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+
+// A device pointer out of a kernel's parameter struct, known to the compiler to point to global memory (such pointers
+// are generic otherwise, and generic accesses also count as LDS operations).
+template <typename T, typename V>
+__device__ __forceinline__ T* global_ptr(V* p) {
+  return (T*)(__attribute__((address_space(1))) T*)(p);
+}
+
+// Eight consecutive elements: a unit of a row, and an operand fragment's share of a lane.
+template <typename T>
+struct Unit {
+  u32x4_t d[sizeof(T) / 2];
+};
+
+// acc += A B over the 32 reduction elements of the wave's fragments: lane l holds elements 8 (l / 16) .. +7 of
+// row (A) or column (B) l % 16, and rows 4 (l / 16) .. +3 of column l % 16 of acc.  fp32: MFMA e multiplies element
+// e of each lane's eight, so the sum runs in another order over the same products.
+__device__ __forceinline__ void mma(f32x4_t& acc, const Unit<bf16_t>& a, const Unit<bf16_t>& b) {
+  acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a.d[0]),
+                                                __builtin_bit_cast(bf16x8_t, b.d[0]), acc, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(f32x4_t& acc, const Unit<float>& a, const Unit<float>& b) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.d[e >> 2][e & 3]), __uint_as_float(b.d[e >> 2][e & 3]),
+                                               acc, 0, 0, 0);
+}
+
+// NE elements at p, of which the first `left` exist (the others read as 0).
+// The loads assume the element's alignment only.
+template <int NE, typename T, typename V>
+__device__ __forceinline__ void load_elems(V& v, const T* p, int64_t left) {
+  static_assert(sizeof(V) == NE * sizeof(T));
+  if (left >= NE) {
+    __builtin_memcpy(&v, p, sizeof(V));
+    return;
+  }
+  T e[NE];
+#pragma unroll
+  for (int i = 0; i < NE; ++i) e[i] = i < left ? p[i] : T{};
+  __builtin_memcpy(&v, e, sizeof(V));
+}
+
+template <typename YT>
+__device__ __forceinline__ void store4(YT* p, const float (&v)[4], int64_t left, bool vec) {
+  if (left <= 0) return;
+  if (vec && left >= 4) {
+    if constexpr (std::is_same<YT, float>::value) {
+      *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
+    } else {
+      *reinterpret_cast<u32x2_t*>(p) =
+          u32x2_t{f32_to_bf16_rne(v[0]) | static_cast<uint32_t>(f32_to_bf16_rne(v[1])) << 16,
+                  f32_to_bf16_rne(v[2]) | static_cast<uint32_t>(f32_to_bf16_rne(v[3])) << 16};
+    }
+    return;
+  }
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (r < left) io<YT>::store(p, r, v[r]);
+}
+
+}  // namespace cci
