@@ -213,6 +213,51 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AParams p, uint32_t no
   }
 }
 
+// expand for few rows: a workgroup has one row and 256 outputs, a lane one
+// output, whose R weights meet T's row in LDS on the vector ALUs (fp32).  A
+// decoding batch has nearly as many adapters as rows, and the matrix cores'
+// walk over a tile's adapters is a chain of memory latencies: 32 rows, 16
+// adapters, 4096 outputs, R = 16: 79 us there.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void expand_rows_kernel(AParams p, uint32_t nob) {
+  extern __shared__ __attribute__((aligned(16))) float t[];  // [R rounded up to 8]
+  const int64_t n = blockIdx.x / nob;
+  const int64_t o = static_cast<int64_t>(blockIdx.x - static_cast<uint32_t>(n) * nob) * kThreads + threadIdx.x;
+  const int32_t a = __builtin_amdgcn_readfirstlane(row_adapter(p, n));
+  float v = 0.0f;
+  if (a >= 0) {
+    const float* part = global_ptr<const float>(p.part);
+    const float s = p.alpha ? global_ptr<const float>(p.alpha)[a] : 1.0f;
+    const int32_t padded = (p.R + 7) & ~7;
+    for (int32_t r = threadIdx.x; r < padded; r += kThreads) {
+      float sum = 0.0f;
+      if (r < p.R)
+        for (int32_t k = 0; k < p.S; ++k) sum += part[(static_cast<int64_t>(k) * p.N + n) * p.R + r];
+      t[r] = sum * s;
+    }
+    __syncthreads();
+    if (o < p.O) {
+      const T* b = global_ptr<const T>(p.B) + (static_cast<int64_t>(a) * p.O + o) * p.R;
+      for (int32_t r = 0; r < p.R; r += 8) {
+        Unit<T> u;
+        load_elems<8>(u, b + r, p.R - r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v = __builtin_fmaf(elem(u, e), t[r + e], v);
+      }
+    }
+  }
+  if (o >= p.O) return;
+  const int64_t at = n * p.O + o;
+  if (p.residual)
+    v += p.d_f32 ? global_ptr<const float>(p.residual)[at] : bf16_to_f32(global_ptr<const uint16_t>(p.residual)[at]);
+  if (p.d_f32)
+    global_ptr<float>(p.D)[at] = v;
+  else
+    global_ptr<uint16_t>(p.D)[at] = f32_to_bf16_rne(v);
+}
+
+constexpr int64_t kFewRows = 64;  // expand on the vector ALUs up to so many rows
+
 // About 512 workgroups: column ranges of at least 256 columns first, then,
 // for a decoding batch's few tiles, workgroups that share the adapters.
 APlan plan(int64_t N, int64_t C, int64_t L) {
@@ -260,6 +305,17 @@ hipError_t launch_adapters(const AdapterArgs& a, hipStream_t s) {
   else
     hipLaunchKernelGGL((shrink_kernel<bf16_t>), grid1, dim3(kThreads), 0, s, p);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (a.N <= kFewRows) {
+    const int64_t blocks = (a.O + kThreads - 1) / kThreads;
+    if (blocks > 0x7fffffff / a.N) return hipErrorInvalidConfiguration;
+    const dim3 grid(static_cast<uint32_t>(a.N * blocks));
+    const size_t lds = static_cast<size_t>((a.R + 7) & ~7) * 4;
+    if (a.t == DType::F32)
+      hipLaunchKernelGGL((expand_rows_kernel<float>), grid, dim3(kThreads), lds, s, p, static_cast<uint32_t>(blocks));
+    else
+      hipLaunchKernelGGL((expand_rows_kernel<bf16_t>), grid, dim3(kThreads), lds, s, p, static_cast<uint32_t>(blocks));
+    return hipGetLastError();
+  }
   if (a.t == DType::F32)
     hipLaunchKernelGGL((expand_kernel<float>), grid2, dim3(kThreads), 0, s, p, static_cast<uint32_t>(nob));
   else

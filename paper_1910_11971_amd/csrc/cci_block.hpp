@@ -38,6 +38,15 @@ struct BlockProduct {
   const void* residual;
   int32_t relu;
 };
+// Groups that meet any `span` rows starting at a multiple of it.
+inline int64_t groups_in(int64_t span, int64_t G) {
+  return span % G == 0 ? span / G : G % span == 0 ? 1 : (span - 2) / G + 2;
+}
+
+// The gated product of few rows (bf16, N <= 64).
+bool gated_few_supports(const BlockProduct& a);
+hipError_t launch_gated_few(const BlockProduct& a, hipStream_t s);
+// Any gated product, plain product, input gradient and packed-value gradient.
 hipError_t launch_tile_gated(const BlockProduct& a, hipStream_t s);
 hipError_t launch_tile_plain(const BlockProduct& a, hipStream_t s);
 hipError_t launch_tile_back(const BlockProduct& a, hipStream_t s);

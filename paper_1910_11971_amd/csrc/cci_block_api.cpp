@@ -140,7 +140,8 @@ cci_status cci_gated_spmm(const void* X, cci_dtype t, int64_t N, int64_t C, cons
   p.act = to_act(act);
   p.Y = H;
   p.pre = pre;
-  return launched(launch_tile_gated(p, static_cast<hipStream_t>(stream)), "gated product");
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  return launched(gated_few_supports(p) ? launch_gated_few(p, st) : launch_tile_gated(p, st), "gated product");
 }
 
 cci_status cci_spmm_t(const void* dY, cci_dtype t, int64_t N, int64_t O, const void* vals, const uint8_t* idx,

@@ -26,6 +26,15 @@ struct Unit {
   u32x4_t d[sizeof(T) / 2];
 };
 
+// Element e of a unit, in fp32.
+template <typename T>
+__device__ __forceinline__ float elem(const Unit<T>& u, int e) {
+  if constexpr (sizeof(T) == 2)
+    return __uint_as_float(e & 1 ? u.d[0][e >> 1] & 0xffff0000u : u.d[0][e >> 1] << 16);
+  else
+    return __uint_as_float(u.d[e >> 2][e & 3]);
+}
+
 // acc += A B over the 32 reduction elements of the wave's fragments: lane l holds elements 8 (l / 16) .. +7 of
 // row (A) or column (B) l % 16, and rows 4 (l / 16) .. +3 of column l % 16 of acc.  fp32: MFMA e multiplies element
 // e of each lane's eight, so the sum runs in another order over the same products.

@@ -11,14 +11,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <typename T>
-__device__ __forceinline__ float elem(const Unit<T>& u, int e) {
-  if constexpr (sizeof(T) == 2)
-    return __uint_as_float(e & 1 ? u.d[0][e >> 1] & 0xffff0000u : u.d[0][e >> 1] << 16);
-  else
-    return __uint_as_float(u.d[e >> 2][e & 3]);
-}
-
 template <typename T, Act A>
 __global__ __launch_bounds__(kThreads) void gate_grad_kernel(const T* __restrict__ dH, const T* __restrict__ pre,
                                                              int64_t N, int64_t F, uint32_t upr, int64_t units,

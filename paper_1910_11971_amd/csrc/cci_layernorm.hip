@@ -24,14 +24,6 @@ constexpr int kFwdThreads = 256;
 constexpr int kBwdThreads = 1024;
 constexpr int kSumCols = 64, kSumGroups = 16;  // reduction of the partial weight gradients
 
-template <typename T>
-__device__ __forceinline__ float elem(const Unit<T>& u, int e) {
-  if constexpr (sizeof(T) == 2)
-    return __uint_as_float(e & 1 ? u.d[0][e >> 1] & 0xffff0000u : u.d[0][e >> 1] << 16);
-  else
-    return __uint_as_float(u.d[e >> 2][e & 3]);
-}
-
 // 8 fp32 values of an optional vector (null: `otherwise`).
 __device__ __forceinline__ void load_vec(float (&v)[8], const float* p, int64_t c, int64_t left, float otherwise) {
   if (p) {

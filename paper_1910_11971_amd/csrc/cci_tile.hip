@@ -25,7 +25,7 @@
 namespace cci {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256;   // of a team
 constexpr int kRowBytes = 128;  // a tile row's chunk in LDS
 constexpr int kGated = 0, kBack = 1, kGrad = 2, kPlain = 3;
 
@@ -78,9 +78,9 @@ struct TParams {
 };
 
 // PL: packed units per lane that are loaded a chunk ahead; 0: more, loaded
-// where they are written.
-template <typename T, int MODE, int TN, int TW, int PL>
-__global__ __launch_bounds__(kThreads, 2) void tile_kernel(TParams p) {
+// where they are written.  TEAMS teams of four waves take turns at the chunks.
+template <typename T, int MODE, int TN, int TW, int PL, int TEAMS>
+__global__ __launch_bounds__(TEAMS * kThreads, TEAMS > 2 ? TEAMS : 2) void tile_kernel(TParams p) {
   constexpr int BK = chunk_of<T>, UPR = BK / 8;  // units of a row's chunk
   constexpr int kXTile = TN * kRowBytes, kWTile = TW * kRowBytes, kBuf = kXTile + kWTile;
   constexpr int TQ = TW / 4;                     // tile rows a wave expands
@@ -88,8 +88,10 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(TParams p) {
   constexpr int XU = TN * UPR / kThreads;        // units of X a thread stages
   constexpr int UC = TQ / 8;                     // back: 8-column units of a packed row in a wave's columns
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x % kThreads, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int team = __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads);
+  uint8_t* bufs = lds + team * (2 * kBuf);  // the team's two buffers
   const int wn = w & 1, wo = w >> 1;
   const T* X = global_ptr<const T>(p.X);
   const T* dY = global_ptr<const T>(p.dY);
@@ -281,20 +283,24 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(TParams p) {
     for (int n = 0; n < NT; ++n) acc[o][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   const uint32_t li = static_cast<uint32_t>(lane & 15), lq = static_cast<uint32_t>(lane >> 4);
 
-  if (nch > 0) {
-    load_chunk(0);
-    store_chunk(lds, 0);
-    if (nch > 1) load_chunk(1);
+  // the team's chunks are team, team + TEAMS, ...; every team makes the same number of rounds (barriers)
+  const int rounds = (nch + TEAMS - 1) / TEAMS;
+  const auto chunk = [&](int i) { return team + TEAMS * i; };
+  if (chunk(0) < nch) {
+    load_chunk(chunk(0));
+    store_chunk(bufs, chunk(0));
+    if (chunk(1) < nch) load_chunk(chunk(1));
   }
 #pragma unroll 1
-  for (int ch = 0; ch < nch; ++ch) {
-    // chunk ch is complete in its buffer, and nobody reads chunk ch - 1's any more
+  for (int i = 0; i < rounds; ++i) {
+    // round i's chunk is complete in its buffer, and nobody reads the one of round i - 1 any more
     lds_barrier();
-    uint8_t* cur = lds + (ch & 1) * kBuf;
-    if (ch + 1 < nch) {
-      store_chunk(lds + ((ch + 1) & 1) * kBuf, ch + 1);
-      if (ch + 2 < nch) load_chunk(ch + 2);
+    const uint8_t* cur = bufs + (i & 1) * kBuf;
+    if (chunk(i + 1) < nch) {
+      store_chunk(bufs + ((i + 1) & 1) * kBuf, chunk(i + 1));
+      if (chunk(i + 2) < nch) load_chunk(chunk(i + 2));
     }
+    if (chunk(i) >= nch) continue;
     const uint8_t* xt = cur;
     const uint8_t* wt = cur + kXTile;
 #pragma unroll
@@ -308,6 +314,30 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(TParams p) {
       for (int o = 0; o < OT; ++o)
 #pragma unroll
         for (int n = 0; n < NT; ++n) mma(acc[o][n], a[o], b[n]);
+    }
+  }
+
+  // ---- the teams' sums, added in their order by the first
+  if constexpr (TEAMS > 1) {
+    lds_barrier();
+    f32x4_t* park = reinterpret_cast<f32x4_t*>(bufs);
+    if (team > 0) {
+#pragma unroll
+      for (int o = 0; o < OT; ++o)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) park[(o * NT + n) * kThreads + tid] = acc[o][n];
+    }
+    lds_barrier();
+    if (team == 0) {
+#pragma unroll
+      for (int t = 1; t < TEAMS; ++t)
+#pragma unroll
+        for (int o = 0; o < OT; ++o)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            acc[o][n] += reinterpret_cast<const f32x4_t*>(lds + t * (2 * kBuf))[(o * NT + n) * kThreads + tid];
+    } else if (MODE != kGrad) {
+      return;
     }
   }
 
@@ -385,12 +415,14 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(TParams p) {
     constexpr int kPitch = TW + 4;
     float* park = reinterpret_cast<float*>(lds);
     lds_barrier();
+    if (team == 0) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int o = 0; o < OT; ++o)
-        *reinterpret_cast<f32x4_t*>(park + (wn * (TN / 2) + 16 * n + li) * kPitch + wo * (TW / 2) + 16 * o + 4 * lq) =
-            acc[o][n];
+        for (int o = 0; o < OT; ++o)
+          *reinterpret_cast<f32x4_t*>(park + (wn * (TN / 2) + 16 * n + li) * kPitch + wo * (TW / 2) + 16 * o + 4 * lq) =
+              acc[o][n];
+    }
     lds_barrier();
     const int64_t o_end = min(w0 + TW, p.O);
     const int64_t g_lo = w0 / p.G;
@@ -399,7 +431,7 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(TParams p) {
     const int c = tid % TN;
     if (n0 + c < p.C) {
 #pragma unroll 1
-      for (int r = tid / TN; r < nrows; r += kThreads / TN) {
+      for (int r = threadIdx.x / TN; r < nrows; r += TEAMS * kThreads / TN) {
         const int64_t at = (g_lo * p.K + r) * p.C + n0 + c;
         const int o = first + (r / p.K) * p.G + static_cast<int>(idx[at]);
         if (o < 0 || o >= lim_o) continue;  // another tile's row
@@ -413,10 +445,10 @@ __global__ __launch_bounds__(kThreads, 2) void tile_kernel(TParams p) {
   }
 }
 
-template <typename T, int MODE, int TN, int TW, int PL>
+template <typename T, int MODE, int TN, int TW, int PL, int TEAMS>
 hipError_t launch(const TParams& q, hipStream_t s) {
   TParams p = q;
-  constexpr int kOperands = 2 * (TN + TW) * kRowBytes;
+  constexpr int kOperands = TEAMS * 2 * (TN + TW) * kRowBytes;
   constexpr int kPark = MODE == kGrad ? TN * (TW + 4) * 4 : 0;
   constexpr int kLds = kOperands > kPark ? kOperands : kPark;
   const int64_t along_n = MODE == kGrad ? p.C : p.N;
@@ -428,29 +460,24 @@ hipError_t launch(const TParams& q, hipStream_t s) {
   p.nwb = static_cast<uint32_t>(nwb);
   p.grid8 = grid % 8 == 0 ? grid / 8 : 0;
   static std::atomic<int8_t> lds_set[kMaxDevices];
-  const hipError_t e = set_lds_limit_once(lds_set, reinterpret_cast<const void*>(&tile_kernel<T, MODE, TN, TW, PL>), kLds);
+  const hipError_t e = set_lds_limit_once(lds_set, reinterpret_cast<const void*>(&tile_kernel<T, MODE, TN, TW, PL, TEAMS>), kLds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((tile_kernel<T, MODE, TN, TW, PL>), dim3(grid), dim3(kThreads), kLds, s, p);
+  hipLaunchKernelGGL((tile_kernel<T, MODE, TN, TW, PL, TEAMS>), dim3(grid), dim3(TEAMS * kThreads), kLds, s, p);
   return hipGetLastError();
 }
 
-// Groups that meet any `span` rows starting at a multiple of it.
-int64_t groups_in(int64_t span, int64_t G) {
-  return span % G == 0 ? span / G : G % span == 0 ? 1 : (span - 2) / G + 2;
-}
-
-template <typename T, int MODE, int TN, int TW>
+template <typename T, int MODE, int TN, int TW, int TEAMS>
 hipError_t launch_pl(const TParams& p, hipStream_t s) {
   if constexpr (MODE == kGrad) {
-    return launch<T, MODE, TN, TW, 0>(p, s);
+    return launch<T, MODE, TN, TW, 0, TEAMS>(p, s);
   } else {
     // packed units of a wave and chunk, per lane
     const int64_t rows = groups_in(MODE == kBack ? chunk_of<T> : TW / 4, p.G) * p.K;
     const int64_t pl = (rows * (MODE == kBack ? TW / 32 : chunk_of<T> / 8) + 63) / 64;
-    if (pl <= 1) return launch<T, MODE, TN, TW, 1>(p, s);
-    if (pl <= 2) return launch<T, MODE, TN, TW, 2>(p, s);
-    if (pl <= 4) return launch<T, MODE, TN, TW, 4>(p, s);
-    return launch<T, MODE, TN, TW, 0>(p, s);
+    if (pl <= 1) return launch<T, MODE, TN, TW, 1, TEAMS>(p, s);
+    if (pl <= 2) return launch<T, MODE, TN, TW, 2, TEAMS>(p, s);
+    if (pl <= 4) return launch<T, MODE, TN, TW, 4, TEAMS>(p, s);
+    return launch<T, MODE, TN, TW, 0, TEAMS>(p, s);
   }
 }
 
@@ -459,7 +486,13 @@ hipError_t launch_tiles(const TParams& p, hipStream_t s) {
   const int64_t an = MODE == kGrad ? p.C : p.N, aw = MODE == kBack ? p.C : p.O;
   // 128 x 128 tiles unless they leave half of the CUs without one
   const int64_t big = (an + 127) / 128 * ((aw + 127) / 128);
-  return big >= 256 ? launch_pl<T, MODE, 128, 128>(p, s) : launch_pl<T, MODE, 64, 64>(p, s);
+  if (big >= 256) return launch_pl<T, MODE, 128, 128, 1>(p, s);
+  // 64 x 64 tiles; up to two a CU, a memory latency per chunk binds, and teams share the chunks (as many as their
+  // registers allow)
+  const int64_t small = (an + 63) / 64 * ((aw + 63) / 64);
+  const int64_t red = MODE == kBack ? p.O : MODE == kGrad ? p.N : p.C;
+  if (small <= 512 && red >= 4 * chunk_of<T>) return launch_pl<T, MODE, 64, 64, sizeof(T) == 2 ? 4 : 2>(p, s);
+  return launch_pl<T, MODE, 64, 64, 1>(p, s);
 }
 
 TParams params(const BlockProduct& a) {
