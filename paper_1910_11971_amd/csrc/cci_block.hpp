@@ -46,11 +46,21 @@ inline int64_t groups_in(int64_t span, int64_t G) {
 // The gated product of few rows (bf16, N <= 64).
 bool gated_few_supports(const BlockProduct& a);
 hipError_t launch_gated_few(const BlockProduct& a, hipStream_t s);
+// Gated products and input gradients that fill the chip with 256-row tiles
+// (bf16; 64 % G == 0, sizes in multiples of 8).
+bool wide_gated_supports(const BlockProduct& a);
+hipError_t launch_wide_gated(const BlockProduct& a, hipStream_t s);
+bool wide_back_supports(const BlockProduct& a);
+hipError_t launch_wide_back(const BlockProduct& a, hipStream_t s);
 // Any gated product, plain product, input gradient and packed-value gradient.
 hipError_t launch_tile_gated(const BlockProduct& a, hipStream_t s);
 hipError_t launch_tile_plain(const BlockProduct& a, hipStream_t s);
 hipError_t launch_tile_back(const BlockProduct& a, hipStream_t s);
 hipError_t launch_tile_grad(const BlockProduct& a, hipStream_t s);
+
+// launch_grad_mfma with the gradient in fp32 or bf16.
+hipError_t launch_grad_mfma_to(const void* dY, const void* X, int64_t N, int64_t C, const uint8_t* idx, int64_t O,
+                               int32_t G, int32_t K, void* dv, DType dv_t, hipStream_t s);
 
 // Gradient of the preactivations of H = act(pre[:, :F]) * pre[:, F:].
 hipError_t launch_gate_grad(const void* dH, const void* pre, DType t, int64_t N, int64_t F, Act act, void* dpre,

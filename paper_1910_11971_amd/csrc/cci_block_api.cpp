@@ -81,6 +81,10 @@ bool tile_product(cci_dtype t, int64_t C, int64_t O, int32_t G) {
   return !mac || (t == CCI_BF16 && (C % 8 != 0 || O % 8 != 0));
 }
 
+hipError_t input_gradient(const BlockProduct& p, hipStream_t st) {
+  return wide_back_supports(p) ? launch_wide_back(p, st) : launch_tile_back(p, st);
+}
+
 }  // namespace
 
 extern "C" {
@@ -141,7 +145,10 @@ cci_status cci_gated_spmm(const void* X, cci_dtype t, int64_t N, int64_t C, cons
   p.Y = H;
   p.pre = pre;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  return launched(gated_few_supports(p) ? launch_gated_few(p, st) : launch_tile_gated(p, st), "gated product");
+  return launched(gated_few_supports(p)    ? launch_gated_few(p, st)
+                  : wide_gated_supports(p) ? launch_wide_gated(p, st)
+                                           : launch_tile_gated(p, st),
+                  "gated product");
 }
 
 cci_status cci_spmm_t(const void* dY, cci_dtype t, int64_t N, int64_t O, const void* vals, const uint8_t* idx,
@@ -166,7 +173,7 @@ cci_status cci_spmm_t(const void* dY, cci_dtype t, int64_t N, int64_t O, const v
   p.K = K;
   p.Y = dX;
   p.y_t = to_dt(dx_t);
-  return launched(launch_tile_back(p, static_cast<hipStream_t>(stream)), "transposed product");
+  return launched(input_gradient(p, static_cast<hipStream_t>(stream)), "transposed product");
 }
 
 cci_status cci_gated_spmm_bwd(const void* dH, const void* pre, const void* X, cci_dtype t, int64_t N, int64_t C,
@@ -199,12 +206,14 @@ cci_status cci_gated_spmm_bwd(const void* dH, const void* pre, const void* X, cc
   if (e == hipSuccess && N > 0 && dX) {
     p.Y = dX;
     p.y_t = p.t;
-    e = launch_tile_back(p, st);
+    e = input_gradient(p, st);
   }
   if (e == hipSuccess && dvals) {
     p.Y = dvals;
     p.y_t = to_dt(dv_t);
-    e = launch_tile_grad(p, st);
+    e = N >= 32 && grad_mfma_supports(dpre, X, p.t, N, C, 2 * F, G)
+            ? launch_grad_mfma_to(dpre, X, N, C, idx, 2 * F, G, K, dvals, p.y_t, st)
+            : launch_tile_grad(p, st);
   }
   return launched(e, "gated backward");
 }

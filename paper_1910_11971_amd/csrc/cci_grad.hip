@@ -30,6 +30,9 @@
 // 0.3 of the 0.85 us) and the matrix cores (0.5 us).  us, with the reads
 // through the compiler's builtin / now: 4096 x 4096 x 4096 177 / 114, 2048 x
 // 2048 x 2048 89 / 27, 4096 samples of 1024 x 1024 173 / 49.
+#include <type_traits>
+
+#include "cci_block.hpp"
 #include "cci_device.hpp"
 #include "cci_launch.hpp"
 
@@ -66,7 +69,7 @@ struct GParams {
   const uint16_t* dY;
   const uint16_t* X;
   const uint8_t* idx;
-  float* dv;
+  void* dv;
   uint32_t dy_bytes, x_bytes;
   int32_t N, C, O, G, K;
   int32_t nob, ncb, nsteps;  // output blocks, column blocks, reduction steps
@@ -151,7 +154,8 @@ __device__ __forceinline__ void read_pair_mfma8(bf16x8_t& f0, bf16x8_t& f1, uint
   f1 = merge(l1, h1);
 }
 
-template <int T>
+// DT: type of the packed gradient (fp32, or bf16 rounded once from the fp32 sum).
+template <int T, typename DT>
 __global__ __launch_bounds__(Tile<T>::kThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void grad_mfma_kernel(GParams p) {
   constexpr int kSide = Tile<T>::kSide, kOpBytes = Tile<T>::kOpBytes, kStage = Tile<T>::kStage;
@@ -325,7 +329,12 @@ void grad_mfma_kernel(GParams p) {
             ix = ix < static_cast<uint32_t>(p.G) ? ix : static_cast<uint32_t>(p.G - 1);
             v[j] = stg[(4 * cq + j) * kEpPitch + gbase + static_cast<int>(ix)];
           }
-          *reinterpret_cast<f32x4_t*>(p.dv + e[x]) = v;
+          if constexpr (std::is_same<DT, float>::value)
+            *reinterpret_cast<f32x4_t*>(static_cast<float*>(p.dv) + e[x]) = v;
+          else
+            *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(p.dv) + e[x]) =
+                u32x2_t{f32_to_bf16_rne(v[0]) | static_cast<uint32_t>(f32_to_bf16_rne(v[1])) << 16,
+                        f32_to_bf16_rne(v[2]) | static_cast<uint32_t>(f32_to_bf16_rne(v[3])) << 16};
         }
       }
     }
@@ -335,7 +344,7 @@ void grad_mfma_kernel(GParams p) {
 // Fewer 256 x 256 tiles than this: 128 x 128 ones, four times as many.
 constexpr int64_t kWideTiles = 160;
 
-template <int T>
+template <int T, typename DT>
 hipError_t launch_grad_t(GParams p, hipStream_t s) {
   constexpr int kSide = Tile<T>::kSide, kLds = Tile<T>::kLdsAll;
   p.nob = (p.O + kSide - 1) / kSide;
@@ -344,9 +353,9 @@ hipError_t launch_grad_t(GParams p, hipStream_t s) {
   if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
   p.grid8 = grid % kXcds == 0 ? static_cast<int32_t>(grid / kXcds) : 0;
   static std::atomic<int8_t> lds_set[kMaxDevices];
-  const hipError_t attr = set_lds_limit_once(lds_set, reinterpret_cast<const void*>(&grad_mfma_kernel<T>), kLds);
+  const hipError_t attr = set_lds_limit_once(lds_set, reinterpret_cast<const void*>(&grad_mfma_kernel<T, DT>), kLds);
   if (attr != hipSuccess) return attr;
-  hipLaunchKernelGGL((grad_mfma_kernel<T>), dim3(static_cast<uint32_t>(grid)), dim3(Tile<T>::kThreads), kLds, s, p);
+  hipLaunchKernelGGL((grad_mfma_kernel<T, DT>), dim3(static_cast<uint32_t>(grid)), dim3(Tile<T>::kThreads), kLds, s, p);
   return hipGetLastError();
 }
 
@@ -363,6 +372,11 @@ bool grad_mfma_supports(const void* dY, const void* X, DType t, int64_t N, int64
 
 hipError_t launch_grad_mfma(const void* dY, const void* X, int64_t N, int64_t C, const uint8_t* idx, int64_t O,
                             int32_t G, int32_t K, float* dv, hipStream_t s) {
+  return launch_grad_mfma_to(dY, X, N, C, idx, O, G, K, dv, DType::F32, s);
+}
+
+hipError_t launch_grad_mfma_to(const void* dY, const void* X, int64_t N, int64_t C, const uint8_t* idx, int64_t O,
+                               int32_t G, int32_t K, void* dv, DType dv_t, hipStream_t s) {
   GParams p{};
   p.dY = static_cast<const uint16_t*>(dY);
   p.X = static_cast<const uint16_t*>(X);
@@ -377,7 +391,9 @@ hipError_t launch_grad_mfma(const void* dY, const void* X, int64_t N, int64_t C,
   p.K = K;
   p.nsteps = static_cast<int32_t>((N + kRows - 1) / kRows);
   const int64_t tiles256 = (O + 255) / 256 * ((C + 255) / 256);
-  return tiles256 >= kWideTiles || 64 % G != 0 ? launch_grad_t<8>(p, s) : launch_grad_t<4>(p, s);
+  const bool wide = tiles256 >= kWideTiles || 64 % G != 0;
+  if (dv_t == DType::BF16) return wide ? launch_grad_t<8, bf16_t>(p, s) : launch_grad_t<4, bf16_t>(p, s);
+  return wide ? launch_grad_t<8, float>(p, s) : launch_grad_t<4, float>(p, s);
 }
 
 }  // namespace cci

@@ -197,7 +197,8 @@ def test_layernorm_bwd_against_differences(cci):
 
 GATED_SIZES = [(1, 8, 8, 8, 2), (1, 64, 96, 16, 4), (3, 5, 6, 3, 2), (16, 128, 256, 16, 4), (17, 33, 40, 4, 1),
                (37, 520, 144, 16, 4), (64, 64, 64, 16, 4), (65, 72, 96, 32, 8), (130, 200, 256, 256, 3),
-               (33, 96, 512, 256, 256), (129, 64, 160, 16, 16), (200, 129, 130, 2, 1), (70, 1000, 48, 8, 8),
+               (33, 96, 512, 256, 256), (129, 64, 160, 16, 16), (200, 129, 130, 2, 1), (70, 1000, 48, 8, 8), (3333, 264, 1736, 8, 2), (1999, 448, 3104, 32, 20), (2500, 1000, 2544, 16, 16),
+               (2048, 512, 2560, 16, 4), (4100, 256, 1536, 64, 4),
                (90, 520, 512, 64, 40), (5, 1, 1, 1, 1), (2049, 136, 1032, 8, 2), (300, 256, 384, 16, 4),
                (2100, 64, 1100, 4, 2), (1024, 320, 2048, 32, 8)]
 
@@ -354,7 +355,8 @@ def test_non_finite_rows_stay_apart(cci):
 
 BACK_SIZES = [(1, 8, 8, 8, 2), (1, 4096, 64, 16, 4), (3, 6, 5, 3, 2), (64, 64, 64, 16, 4), (33, 96, 129, 32, 8),
               (100, 512, 200, 256, 7), (70, 256, 264, 256, 256), (2049, 72, 2050, 8, 2), (2048, 512, 2048, 16, 4),
-              (300, 1040, 512, 16, 16), (257, 130, 131, 2, 1), (90, 960, 256, 64, 33), (40, 21, 1, 7, 3)]
+              (300, 1040, 512, 16, 16), (3333, 1736, 3400, 8, 2), (6001, 400, 2056, 16, 9),
+              (4096, 320, 3136, 2, 1), (4000, 640, 4000, 64, 64), (8192, 256, 1792, 16, 1), (257, 130, 131, 2, 1), (90, 960, 256, 64, 33), (40, 21, 1, 7, 3)]
 
 
 @DTYPES
