@@ -416,7 +416,8 @@ cci_status cci_global_avgpool_nhwc(const void *X, cci_dtype x_t, int64_t B,
  * layer norm, the gated product of two CCI projections, the input gradient
  * of a CCI product for any G and K, and low-rank adapters beside a shared
  * CCI projection.  Each computes one type t throughout (F32 or BF16, weights
- * included) with fp32 sums; any sizes; rows need no alignment of their own.
+ * included) with fp32 sums, for any sizes (products: C, O and 2F up to 2^20);
+ * rows need no alignment of their own.
  * ------------------------------------------------------------------------ */
 
 /* Layer norm of each row of X [N][C]:

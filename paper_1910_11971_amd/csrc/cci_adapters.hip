@@ -66,7 +66,7 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(AParams p) {
   const int32_t sl = static_cast<int32_t>(rest / p.P), turn = static_cast<int32_t>(rest % p.P);
   const int64_t n = static_cast<int64_t>(tile) * kRows + li;
   const int64_t c_lo = sl * p.cols, c_hi = min(p.C, c_lo + p.cols);
-  const T* x = global_ptr<const T>(p.X) + n * p.C;
+  const T* x = global_ptr<const T>(p.X) + min(n, p.N - 1) * p.C;  // (rows past the last have no adapter)
   const T* A = global_ptr<const T>(p.A);
   float* part = global_ptr<float>(p.part);
   const int32_t mine = row_adapter(p, n);
@@ -82,14 +82,15 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(AParams p) {
       for (int b = 0; b < kRankBlocks; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       const int nb = min(kRankBlocks, rank_blocks - rb0);
       const int64_t r0 = 16 * rb0 + li;
-      const T* ar = A + (static_cast<int64_t>(a) * p.R + r0) * p.C;
+      const T* ar = A + static_cast<int64_t>(a) * p.R * p.C;
       for (int64_t c0 = c_lo + 32 * w; c0 < c_hi; c0 += 32 * kWaves) {
         const int64_t c = c0 + 8 * lq, left = p.C - c;
+        const bool whole = c0 + 32 <= p.C;
         Unit<T> xf, af[kRankBlocks];
-        load_elems<8>(xf, x + c, n < p.N ? left : 0);
+        load_part<8>(xf, x + c, left, whole);
 #pragma unroll
-        for (int b = 0; b < kRankBlocks; ++b)
-          if (b < nb) load_elems<8>(af[b], ar + 16 * b * p.C + c, r0 + 16 * b < p.R ? left : 0);
+        for (int b = 0; b < kRankBlocks; ++b)  // (ranks past the last read it again: their sums are not stored)
+          if (b < nb) load_part<8>(af[b], ar + min(r0 + 16 * b, static_cast<int64_t>(p.R - 1)) * p.C + c, left, whole);
 #pragma unroll
         for (int b = 0; b < kRankBlocks; ++b)
           if (b < nb) mma(acc[b], af[b], xf);
@@ -170,8 +171,8 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AParams p, uint32_t no
       Unit<T> bf[kOutBlocks];
 #pragma unroll
       for (int b = 0; b < kOutBlocks; ++b) {
-        const int64_t o = o0 + 16 * b + li;
-        load_elems<8>(bf[b], B + (static_cast<int64_t>(a) * p.O + o) * p.R + r0, o < p.O ? p.R - r0 : 0);
+        const int64_t o = min(o0 + 16 * b + li, p.O - 1);  // (outputs past the last are not stored)
+        load_elems<8>(bf[b], B + (static_cast<int64_t>(a) * p.O + o) * p.R + r0, p.R - r0);
       }
       if constexpr (sizeof(T) == 2) {
         const Split q = split(t);

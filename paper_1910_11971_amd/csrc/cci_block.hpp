@@ -43,15 +43,17 @@ inline int64_t groups_in(int64_t span, int64_t G) {
   return span % G == 0 ? span / G : G % span == 0 ? 1 : (span - 2) / G + 2;
 }
 
-// The gated product of few rows (bf16, N <= 64).
-bool gated_few_supports(const BlockProduct& a);
-hipError_t launch_gated_few(const BlockProduct& a, hipStream_t s);
-// Gated products and input gradients that fill the chip with 256-row tiles
-// (bf16; 64 % G == 0, sizes in multiples of 8).
+// bf16 gated products and input gradients over few tiles of up to 64 rows x
+// 16 wb weight rows (wb 4, 2; input gradients also 1): 8 wb outputs (gated) or
+// 16 wb columns.
+bool wave_split_supports(const BlockProduct& a, bool gated, int wb);
+hipError_t launch_wave_split(const BlockProduct& a, bool gated, int wb, hipStream_t s);
+// bf16 gated products and input gradients in tiles of 32 pt rows (pt 4 or 8)
+// x 128 outputs (gated) or 256 columns; 64 % G == 0, sizes in multiples of 8.
 bool wide_gated_supports(const BlockProduct& a);
-hipError_t launch_wide_gated(const BlockProduct& a, hipStream_t s);
+hipError_t launch_wide_gated(const BlockProduct& a, int pt, hipStream_t s);
 bool wide_back_supports(const BlockProduct& a);
-hipError_t launch_wide_back(const BlockProduct& a, hipStream_t s);
+hipError_t launch_wide_back(const BlockProduct& a, int pt, hipStream_t s);
 // Any gated product, plain product, input gradient and packed-value gradient.
 hipError_t launch_tile_gated(const BlockProduct& a, hipStream_t s);
 hipError_t launch_tile_plain(const BlockProduct& a, hipStream_t s);

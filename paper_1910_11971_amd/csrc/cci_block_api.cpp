@@ -3,6 +3,8 @@
 // state.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "../../include/cci.h"
 #include "cci_block.hpp"
 #include "cci_check.hpp"
@@ -16,6 +18,16 @@ cci_status check_rows(int64_t N, int64_t width) {
   if (N < 0) return fail(CCI_EINVAL, "N=%lld < 0", (long long)N);
   if (N > (int64_t(1) << 31) || N > (int64_t(1) << 40) / width) return fail(CCI_EINVAL, "N too large");
   return CCI_OK;
+}
+
+// Lanes of the product kernels address rows with 32-bit offsets.
+constexpr int64_t kWidest = int64_t(1) << 20;
+
+cci_status check_product(int64_t N, int64_t C, int64_t O, int32_t G, int32_t K) {
+  if (cci_status s = check_groups(O, C, G, K)) return s;
+  if (C > kWidest || O > kWidest)
+    return fail(CCI_EINVAL, "C=%lld or %lld weight rows above 2^20", (long long)C, (long long)O);
+  return check_rows(N, C > O ? C : O);
 }
 
 cci_status check_act(cci_act act) {
@@ -45,9 +57,8 @@ cci_status check_norm(cci_dtype t, int64_t N, int64_t C) {
 cci_status check_gated(cci_dtype t, int64_t N, int64_t C, int64_t F, int32_t G, int32_t K, cci_act act) {
   if (!dtype_ok(t)) return fail(CCI_EINVAL, "unknown dtype code");
   if (cci_status s = check_groups(F, C, G, K)) return s;
-  if (cci_status s = check_groups(2 * F, C, G, K)) return s;
   if (cci_status s = check_act(act)) return s;
-  return check_rows(N, C > 2 * F ? C : 2 * F);
+  return check_product(N, C, 2 * F, G, K);
 }
 
 Act to_act(cci_act a) {
@@ -81,8 +92,81 @@ bool tile_product(cci_dtype t, int64_t C, int64_t O, int32_t G) {
   return !mac || (t == CCI_BF16 && (C % 8 != 0 || O % 8 != 0));
 }
 
+// ---------------------------------------------------------------------------
+// Which kernels run a bf16 gated product or input gradient.  Each family has a
+// time per piece of the reduction and round of workgroups over the 256 CUs,
+// measured on 90 shapes with G = 4 .. 32 and K / G = 1/4 and 1/2 (us):
+//   64 x 64 tiles, four teams of waves  1.3 a 4 chunks of 64, 3.5 a round
+//   64 x 64 tiles, one team             0.95 a chunk for up to 1024 tiles
+//   128 x 128 tiles                     1.1 a chunk, 1.4 for 257 .. 512 tiles, and so on by 512
+//   wide tiles, 128 rows                1.07 a chunk, 256 rows 1.42
+//   wave-split                          0.3 per row block and 32 elements of a step of its eight waves, 0.55 at
+//                                       least, 4 a round
+// Both sides of the borders (tile / wide 128 / wide 256 / wave-split):
+//   gated, C = 4096, F = 8192: 128 rows 48 / 68 / 94 / 51, 256 rows 70 / 69 / 95 / 96, 1024 rows 171 / 134 / 103 / 360;
+//   dX, O = 8192, C = 4096: 256 rows 50 / 136 / 182 / 45, 1024 rows 144 / 137 / 181 / 164, 2048 rows 190 / 142 / 181 / 309.
+
+double rounds(int64_t tiles, int64_t at_once) { return static_cast<double>((tiles + at_once - 1) / at_once); }
+
+enum Kind { kTiles, kWide128, kWide256, kWave4, kWave2, kWave1 };
+struct Choice {
+  Kind kind;
+  double us;
+};
+void consider(Choice& best, Kind kind, double us) {
+  if (us < best.us) best = Choice{kind, us};
+}
+
+// out: the outputs of a row, per64 / per256: those of a 64- and a 256-row weight tile.
+Choice tile_or_wide(const BlockProduct& p, int64_t red, int64_t out, int64_t per64, int64_t per256, bool wide) {
+  const double chunks = static_cast<double>((red + 63) / 64);
+  const int64_t t64 = (p.N + 63) / 64 * ((out + per64 - 1) / per64);
+  const int64_t t128 = (p.N + 127) / 128 * ((out + 2 * per64 - 1) / (2 * per64));
+  const double teams = static_cast<double>((red + 255) / 256);
+  Choice best{kTiles, 4.0 + (t128 >= 256   ? chunks * (t128 <= 256 ? 1.1 : 1.4 * rounds(t128, 512))
+                        : t64 <= 512 ? rounds(t64, 256) * (teams * 1.3 + 3.5)
+                                     : chunks * 0.95)};
+  if (wide) {
+    const int64_t w = (out + per256 - 1) / per256;
+    consider(best, kWide128, 4.0 + chunks * 1.07 * rounds((p.N + 127) / 128 * w, 256));
+    consider(best, kWide256, 6.0 + chunks * 1.42 * rounds((p.N + 255) / 256 * w, 256));
+  }
+  return best;
+}
+
+// The best of the wave-split kernels' tile widths.
+void consider_wave_split(Choice& best, const BlockProduct& p, bool gated) {
+  const int64_t red = gated ? p.C : p.O, out = gated ? p.O / 2 : p.C;
+  const int64_t nt = p.N <= 16 ? 1 : p.N <= 32 ? 2 : 4;  // blocks of 16 rows
+  for (const int wb : {4, 2, 1}) {
+    if (!wave_split_supports(p, gated, wb)) continue;
+    const int64_t ks = 128 / wb;  // elements of a step
+    const double step = std::max(0.55, 0.3 * static_cast<double>(nt * ks / 32));
+    const double steps = static_cast<double>((red + 8 * ks - 1) / (8 * ks));
+    const int64_t width = (gated ? 8 : 16) * wb, tiles = (p.N + 16 * nt - 1) / (16 * nt) * ((out + width - 1) / width);
+    consider(best, wb == 4 ? kWave4 : wb == 2 ? kWave2 : kWave1, 5.0 + rounds(tiles, 256) * (steps * step + 4.0));
+  }
+}
+
+int wave_width(Kind kind) { return kind == kWave4 ? 4 : kind == kWave2 ? 2 : kind == kWave1 ? 1 : 0; }
+
+hipError_t gated_product(const BlockProduct& p, hipStream_t st) {
+  if (p.t != DType::BF16) return launch_tile_gated(p, st);
+  // (Beyond a decoding batch the rows of X that a wave-split workgroup reads in fragments cost as much as they save:
+  // C = 4096, F = 8192: 32 rows 17 / 25 on 64 x 64 tiles, 64 rows 27 / 25; odd C more.)
+  Choice c{kTiles, 1e30};
+  if (p.N <= 32) consider_wave_split(c, p, true);
+  if (c.kind == kTiles) c = tile_or_wide(p, p.C, p.O / 2, 32, 128, wide_gated_supports(p));
+  if (const int wb = wave_width(c.kind)) return launch_wave_split(p, true, wb, st);
+  return c.kind == kTiles ? launch_tile_gated(p, st) : launch_wide_gated(p, c.kind == kWide256 ? 8 : 4, st);
+}
+
 hipError_t input_gradient(const BlockProduct& p, hipStream_t st) {
-  return wide_back_supports(p) ? launch_wide_back(p, st) : launch_tile_back(p, st);
+  if (p.t != DType::BF16) return launch_tile_back(p, st);
+  Choice c = tile_or_wide(p, p.O, p.C, 64, 256, wide_back_supports(p));
+  consider_wave_split(c, p, false);
+  if (const int wb = wave_width(c.kind)) return launch_wave_split(p, false, wb, st);
+  return c.kind == kTiles ? launch_tile_back(p, st) : launch_wide_back(p, c.kind == kWide256 ? 8 : 4, st);
 }
 
 }  // namespace
@@ -145,18 +229,14 @@ cci_status cci_gated_spmm(const void* X, cci_dtype t, int64_t N, int64_t C, cons
   p.Y = H;
   p.pre = pre;
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  return launched(gated_few_supports(p)    ? launch_gated_few(p, st)
-                  : wide_gated_supports(p) ? launch_wide_gated(p, st)
-                                           : launch_tile_gated(p, st),
-                  "gated product");
+  return launched(gated_product(p, st), "gated product");
 }
 
 cci_status cci_spmm_t(const void* dY, cci_dtype t, int64_t N, int64_t O, const void* vals, const uint8_t* idx,
                       int64_t C, int32_t G, int32_t K, void* dX, cci_dtype dx_t, void* stream) {
   if (!dtype_ok(t) || !dtype_ok(dx_t)) return fail(CCI_EINVAL, "unknown dtype code");
   if (t == CCI_F32 && dx_t != CCI_F32) return fail(CCI_EUNSUPPORTED, "an fp32 product has an fp32 output");
-  if (cci_status s = check_groups(O, C, G, K)) return s;
-  if (cci_status s = check_rows(N, C > O ? C : O)) return s;
+  if (cci_status s = check_product(N, C, O, G, K)) return s;
   if (N == 0) return ok();
   if (!dY || !vals || !idx || !dX) return fail(CCI_EINVAL, "null pointer");
   if (!aligned16(dY) || !aligned16(vals) || !aligned16(idx) || !aligned16(dX))
@@ -234,7 +314,7 @@ cci_status cci_spmm_adapters(const void* X, cci_dtype x_t, int64_t N, int64_t C,
   if (!dtype_ok(x_t) || !dtype_ok(val_t) || !dtype_ok(y_t)) return fail(CCI_EINVAL, "unknown dtype code");
   if (x_t != val_t || (x_t == CCI_F32 && y_t != CCI_F32))
     return fail(CCI_EUNSUPPORTED, "dtype combination (x=%d, vals=%d, y=%d) not supported", x_t, val_t, y_t);
-  if (cci_status s = check_groups(O, C, G, K)) return s;
+  if (cci_status s = check_product(N, C, O, G, K)) return s;
   if (!adapters) return fail(CCI_EINVAL, "null pointer");
   if (cci_status s = check_adapters(N, C, O, adapters->L, adapters->R)) return s;
   if (N == 0) return ok();

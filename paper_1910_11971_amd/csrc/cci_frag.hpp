@@ -35,6 +35,26 @@ __device__ __forceinline__ float elem(const Unit<T>& u, int e) {
     return __uint_as_float(u.d[e >> 2][e & 3]);
 }
 
+// A unit's eight entries in another order: what is entry e becomes entry e ^ m,
+// m a lane's own.  The lanes of a wave write their entries one at a time; in
+// the same order they would meet in few banks of the LDS.
+struct Shuffle {
+  uint32_t m, bytes, half;
+};
+__device__ __forceinline__ Shuffle make_shuffle(uint32_t m) {
+  return Shuffle{m, 0x03020100u ^ (0x01010101u * (m & 3u)), 16u * (m & 1u)};
+}
+__device__ __forceinline__ void shuffle(const Shuffle& s, Unit<bf16_t>& v, u32x2_t& ix) {
+  const bool s1 = (s.m & 2u) != 0, s2 = (s.m & 4u) != 0;
+  u32x4_t a = v.d[0];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) a[j] = __builtin_amdgcn_alignbit(a[j], a[j], s.half);
+  const u32x4_t b = s1 ? u32x4_t{a[1], a[0], a[3], a[2]} : a;
+  v.d[0] = s2 ? u32x4_t{b[2], b[3], b[0], b[1]} : b;
+  const uint32_t lo = __builtin_amdgcn_perm(ix[0], ix[0], s.bytes), hi = __builtin_amdgcn_perm(ix[1], ix[1], s.bytes);
+  ix = s2 ? u32x2_t{hi, lo} : u32x2_t{lo, hi};
+}
+
 // acc += A B over the 32 reduction elements of the wave's fragments: lane l holds elements 8 (l / 16) .. +7 of
 // row (A) or column (B) l % 16, and rows 4 (l / 16) .. +3 of column l % 16 of acc.  fp32: MFMA e multiplies element
 // e of each lane's eight, so the sum runs in another order over the same products.
@@ -49,19 +69,43 @@ __device__ __forceinline__ void mma(f32x4_t& acc, const Unit<float>& a, const Un
                                                acc, 0, 0, 0);
 }
 
-// NE elements at p, of which the first `left` exist (the others read as 0).
-// The loads assume the element's alignment only.
+// NE elements at p.  Rows need no alignment beyond their element's.
 template <int NE, typename T, typename V>
-__device__ __forceinline__ void load_elems(V& v, const T* p, int64_t left) {
+__device__ __forceinline__ void load_full(V& v, const T* p) {
   static_assert(sizeof(V) == NE * sizeof(T));
-  if (left >= NE) {
-    __builtin_memcpy(&v, p, sizeof(V));
-    return;
-  }
+  __builtin_memcpy(&v, p, sizeof(V));
+}
+// The same where only the first `left` exist and the others read as 0: one
+// load per element, those past the row's end from its last element (which is
+// p[left - 1], also for left <= 0), and no branch.
+template <int NE, typename T, typename V>
+__device__ __forceinline__ void load_tail(V& v, const T* p, int64_t left) {
+  static_assert(sizeof(V) == NE * sizeof(T));
   T e[NE];
 #pragma unroll
-  for (int i = 0; i < NE; ++i) e[i] = i < left ? p[i] : T{};
+  for (int i = 0; i < NE; ++i) e[i] = p[i < left ? i : left - 1];
+#pragma unroll
+  for (int i = 0; i < NE; ++i) e[i] = i < left ? e[i] : T{};
   __builtin_memcpy(&v, e, sizeof(V));
+}
+// Either, by `whole`, which is uniform over a wave: a branch that no lane of a
+// whole chunk pays for.
+template <int NE, typename T, typename V>
+__device__ __forceinline__ void load_part(V& v, const T* p, int64_t left, bool whole) {
+  if (whole)
+    load_full<NE>(v, p);
+  else
+    load_tail<NE>(v, p, left);
+}
+// By lane: all of them, a part, or none (left <= 0: nothing is read).
+template <int NE, typename T, typename V>
+__device__ __forceinline__ void load_elems(V& v, const T* p, int64_t left) {
+  if (left >= NE) {
+    load_full<NE>(v, p);
+  } else {
+    v = V{};
+    if (left > 0) load_tail<NE>(v, p, left);
+  }
 }
 
 template <typename YT>

@@ -33,16 +33,12 @@ template <typename T> constexpr int chunk_of = kRowBytes / static_cast<int>(size
 
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// LDS: element (row, k) of a tile sits in 16-byte slot k sizeof(T) / 16 of the
-// row's 128 bytes, the slot XOR-ed with (row / 2) % 8, so that the 16 rows of
-// a fragment read touch distinct bank slots.
+// LDS layouts of a chunk, 128 bytes a row.
+// Rows that are staged whole: 16-byte slot i of a row at slot i ^ (row / 2) % 8
+// of its 128 bytes, so that the 16 rows of a fragment read touch distinct bank
+// slots.
 __device__ __forceinline__ uint32_t slot_addr(uint32_t row, uint32_t slot) {
   return row * kRowBytes + ((slot ^ ((row >> 1) & 7u)) << 4);
-}
-template <typename T>
-__device__ __forceinline__ uint32_t elem_addr(uint32_t row, uint32_t k) {
-  const uint32_t b = k * static_cast<uint32_t>(sizeof(T));
-  return slot_addr(row, b >> 4) + (b & 15u);
 }
 template <typename T>
 __device__ __forceinline__ Unit<T> read_unit(const uint8_t* tile, uint32_t row, uint32_t u) {
@@ -57,6 +53,24 @@ __device__ __forceinline__ void write_unit(uint8_t* tile, uint32_t row, uint32_t
 #pragma unroll
   for (uint32_t h = 0; h < sizeof(T) / 2; ++h)
     *reinterpret_cast<u32x4_t*>(tile + slot_addr(row, u * (sizeof(T) / 2) + h)) = f.d[h];
+}
+// The expanded weights, written entry by entry: 16-byte slots of 16 rows side
+// by side, erow(row) + ecol(k).  A fragment read is 1 KiB in a row, and with
+// whole groups in a tile an entry's address is its group's plus a shift of its
+// index.
+__device__ __forceinline__ uint32_t erow(uint32_t row) { return ((row >> 4) << 11) | ((row & 15u) << 4); }
+template <typename T>
+__device__ __forceinline__ uint32_t ecol(uint32_t k) {
+  const uint32_t b = k * static_cast<uint32_t>(sizeof(T));
+  return ((b >> 4) << 8) | (b & 15u);
+}
+template <typename T>
+__device__ __forceinline__ Unit<T> read_expanded(const uint8_t* tile, uint32_t block, uint32_t u, uint32_t li) {
+  Unit<T> f;
+#pragma unroll
+  for (uint32_t h = 0; h < sizeof(T) / 2; ++h)
+    f.d[h] = *reinterpret_cast<const u32x4_t*>(tile + (block << 11) + ((u * (sizeof(T) / 2) + h) << 8) + (li << 4));
+  return f;
 }
 
 struct TParams {
@@ -114,24 +128,44 @@ __global__ __launch_bounds__(TEAMS * kThreads, TEAMS > 2 ? TEAMS : 2) void tile_
   const int64_t ldx = MODE == kBack ? p.O : p.C;
   const int nch = static_cast<int>((red + BK - 1) / BK);
 
-  // ---- staging of X (gated, back: rows n0 .. of the reduction operand)
-  Unit<T> xu[MODE == kGrad ? 1 : XU];
-  auto load_x = [&](int ch) __attribute__((always_inline)) {
-    if constexpr (MODE != kGrad) {
+  // Loads run ND chunks ahead of their use, in register sets taken in turn
+  // (one set where two do not fit the registers).
+  constexpr int ND = (MODE == kGrad || PL == 4) && (sizeof(T) == 4 || TEAMS == 4) ? 1 : 2;
+
+  // ---- staging of X (gated, plain, back: rows n0 .. of the reduction operand).
+  // Rows past the last read it again: their outputs are not stored.  Offsets
+  // of lanes are 32-bit, from a row block's first row.
+  Unit<T> xu[ND][MODE == kGrad ? 1 : XU];
+  const char* xbase = reinterpret_cast<const char*>(X + (MODE == kGrad ? 0 : n0 * ldx));
+  uint32_t xoff[MODE == kGrad ? 1 : XU];
+  if constexpr (MODE != kGrad) {
 #pragma unroll
-      for (int i = 0; i < XU; ++i) {
-        const int v = tid + kThreads * i, row = v / UPR, u = v % UPR;
-        const int64_t k = static_cast<int64_t>(ch) * BK + 8 * u;
-        load_elems<8>(xu[i], X + (n0 + row) * ldx + k, n0 + row < p.N ? red - k : 0);
+    for (int i = 0; i < XU; ++i) {
+      const int v = tid + kThreads * i;
+      const uint32_t row = static_cast<uint32_t>(min(static_cast<int64_t>(v / UPR), p.N - 1 - n0));
+      xoff[i] = (row * static_cast<uint32_t>(ldx) + 8u * (v % UPR)) * static_cast<uint32_t>(sizeof(T));
+    }
+  }
+  auto load_x = [&](int ch, int set) __attribute__((always_inline)) {
+    if constexpr (MODE != kGrad) {
+      const char* xc = xbase + static_cast<int64_t>(ch) * kRowBytes;
+      if ((ch + 1) * static_cast<int64_t>(BK) <= red) {
+#pragma unroll
+        for (int i = 0; i < XU; ++i) load_full<8>(xu[set][i], reinterpret_cast<const T*>(xc + xoff[i]));
+      } else {
+#pragma unroll
+        for (int i = 0; i < XU; ++i)
+          load_tail<8>(xu[set][i], reinterpret_cast<const T*>(xc + xoff[i]),
+                       red - static_cast<int64_t>(ch) * BK - 8 * ((tid + kThreads * i) % UPR));
       }
     }
   };
-  auto store_x = [&](uint8_t* buf) __attribute__((always_inline)) {
+  auto store_x = [&](uint8_t* buf, int set) __attribute__((always_inline)) {
     if constexpr (MODE != kGrad) {
 #pragma unroll
       for (int i = 0; i < XU; ++i) {
         const int v = tid + kThreads * i;
-        write_unit<T>(buf, static_cast<uint32_t>(v / UPR), static_cast<uint32_t>(v % UPR), xu[i]);
+        write_unit<T>(buf, static_cast<uint32_t>(v / UPR), static_cast<uint32_t>(v % UPR), xu[set][i]);
       }
     }
   };
@@ -139,19 +173,31 @@ __global__ __launch_bounds__(TEAMS * kThreads, TEAMS > 2 ? TEAMS : 2) void tile_
   // ---- grad: both operands are sample-major; a thread loads 4 columns of 8
   // samples and writes them transposed, 8 samples of a column to a unit.
   using Quad = std::conditional_t<sizeof(T) == 2, u32x2_t, u32x4_t>;
-  Quad qx[MODE == kGrad ? 8 : 1], qy[MODE == kGrad ? 8 : 1];
-  auto load_quads = [&](Quad (&q)[MODE == kGrad ? 8 : 1], const T* src, int64_t width, int64_t col0, int cols, int ch) __attribute__((always_inline)) {
+  constexpr int kQuads = MODE == kGrad ? 8 : 1;
+  Quad qx[ND][kQuads], qy[ND][kQuads];
+  auto load_quads = [&](Quad (&q)[kQuads], const T* src, int64_t width, int64_t col0, int cols, int ch) __attribute__((always_inline)) {
     if constexpr (MODE == kGrad) {
-      const int cq = tid % (cols / 4), rg = tid / (cols / 4);
-      const int64_t c = col0 + 4 * cq;
+      const int cq = tid % (cols / 4), rg = min(tid / (cols / 4), UPR - 1);
+      const char* qb = reinterpret_cast<const char*>(src + static_cast<int64_t>(ch) * BK * width + col0);
+      const bool all = (ch + 1) * static_cast<int64_t>(BK) <= p.N;
+      const int last = all ? BK - 1 : static_cast<int>(p.N - 1 - static_cast<int64_t>(ch) * BK);  // sample of the chunk
+      if (all && col0 + cols <= width) {
+        const uint32_t off = (static_cast<uint32_t>(8 * rg) * static_cast<uint32_t>(width) + 4u * cq) * static_cast<uint32_t>(sizeof(T));
+        const uint32_t step = static_cast<uint32_t>(width) * static_cast<uint32_t>(sizeof(T));
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const int64_t n = static_cast<int64_t>(ch) * BK + 8 * rg + r;
-        load_elems<4>(q[r], src + n * width + c, n < p.N && rg < UPR ? width - c : 0);
+        for (int r = 0; r < 8; ++r) load_full<4>(q[r], reinterpret_cast<const T*>(qb + (off + r * step)));
+      } else {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const uint32_t off = (static_cast<uint32_t>(min(8 * rg + r, last)) * static_cast<uint32_t>(width) + 4u * cq) *
+                               static_cast<uint32_t>(sizeof(T));
+          load_tail<4>(q[r], reinterpret_cast<const T*>(qb + off), width - col0 - 4 * cq);
+          if (8 * rg + r > last) q[r] = Quad{};  // a sample past the last adds nothing
+        }
       }
     }
   };
-  auto store_quads = [&](uint8_t* tile, const Quad (&q)[MODE == kGrad ? 8 : 1], int cols) __attribute__((always_inline)) {
+  auto store_quads = [&](uint8_t* tile, const Quad (&q)[kQuads], int cols) __attribute__((always_inline)) {
     if constexpr (MODE == kGrad) {
       const int cq = tid % (cols / 4), rg = tid / (cols / 4);
       if (rg < UPR) {
@@ -178,101 +224,155 @@ __global__ __launch_bounds__(TEAMS * kThreads, TEAMS > 2 ? TEAMS : 2) void tile_
   // from the first group that meets its rows (gated, plain) or the chunk (back).
   // Entry e of it goes to (tile row, reduction element)
   //   gated, plain (row0 + idx[e], 8 u + e) if row0 + idx[e] is among the wave's rows,
-  //   back         (8 u + e, row0 + idx[e]) if row0 + idx[e] is in the chunk.
+  //   back         (8 u + e, row0 + idx[e]) if row0 + idx[e] is in the chunk,
+  // and otherwise to a word that nobody reads.
+  constexpr int kUnitsOfRow = MODE == kBack ? UC : UPR;
   const int64_t f0 = w0 + (MODE == kGated ? (w >> 1) * TQ : w * TQ);  // gated, plain: the wave's first output
   const int64_t wrow = f0 + (MODE == kGated && (w & 1) ? F : 0);      // and weight row
   const int64_t rest = max((MODE == kGated ? F : p.O) - f0, static_cast<int64_t>(0));
-  const int lim = kFwd ? static_cast<int>(min(static_cast<int64_t>(TQ), rest)) : BK;
+  const uint32_t lim = kFwd ? static_cast<uint32_t>(min(static_cast<int64_t>(TQ), rest)) : BK;
   constexpr int PU = PL > 0 ? PL : 1;
-  Unit<T> pv[PU];
-  u32x2_t pi[PU];
-  int gl[PU];  // group of the unit's packed row, from the first
+  Unit<T> pv[ND][PU];
+  u32x2_t pi[ND][PU];
+  int grow[PU];  // first row of the group of the unit's packed row, from the first group's
 #pragma unroll
-  for (int i = 0; i < PU; ++i) gl[i] = (lane + 64 * i) / (MODE == kBack ? UC : UPR) / p.K;
+  for (int i = 0; i < PU; ++i) grow[i] = (lane + 64 * i) / kUnitsOfRow / p.K * p.G;
   struct Span {
-    int64_t g_lo;  // first group
-    int nrows;     // packed rows
-    int first;     // g_lo G relative to the wave's rows / the chunk
+    uint32_t g_lo;  // first group
+    int nrows;      // packed rows
+    int first;      // g_lo G relative to the wave's rows / the chunk
   };
-  auto span = [&](int ch) __attribute__((always_inline)) {
-    const int64_t b = kFwd ? wrow : static_cast<int64_t>(ch) * BK;
-    const int64_t last = kFwd ? b + lim - 1 : min(b + BK, p.O) - 1;
-    Span s;
-    s.g_lo = b / p.G;
-    s.nrows = last >= b ? static_cast<int>(last / p.G - s.g_lo + 1) * p.K : 0;
-    s.first = static_cast<int>(s.g_lo * p.G - b);
+  auto span = [&](uint32_t b, uint32_t n) __attribute__((always_inline)) {  // groups that meet rows b .. b + n - 1
+    const uint32_t G = static_cast<uint32_t>(p.G);
+    Span s{0, 0, 0};
+    if (n > 0) {
+      s.g_lo = b / G;
+      s.nrows = static_cast<int>((b + n - 1) / G - s.g_lo + 1) * p.K;
+      s.first = static_cast<int>(s.g_lo * G) - static_cast<int>(b);
+    }
     return s;
   };
-  const Span gspan = span(0);  // (gated, plain: the same in every chunk)
-  auto load_unit = [&](const Span& s, int ch, int v, Unit<T>& val, u32x2_t& ix) __attribute__((always_inline)) {
-    const int r = v / (MODE == kBack ? UC : UPR), u = v % (MODE == kBack ? UC : UPR);
-    const int64_t c = kFwd ? static_cast<int64_t>(ch) * BK + 8 * u : w0 + w * TQ + 8 * u;
-    const int64_t at = (s.g_lo * p.K + r) * p.C + c;
-    const int64_t left = r < s.nrows ? p.C - c : 0;
-    load_elems<8>(val, vals + at, left);
-    load_elems<8>(ix, idx + at, left);
+  // (gated, plain: the same in every chunk.  back: where G divides the chunk, the next chunk's groups follow)
+  const Span span0 = kFwd ? span(static_cast<uint32_t>(wrow), lim) : span(0, min(static_cast<uint32_t>(BK), static_cast<uint32_t>(p.O)));
+  const int gpc = MODE == kBack && BK % p.G == 0 ? BK / p.G : 0;  // back: groups per chunk
+  auto span_of = [&](int ch) __attribute__((always_inline)) {
+    if constexpr (kFwd) return span0;
+    const uint32_t b = static_cast<uint32_t>(ch) * BK, n = min(static_cast<uint32_t>(BK), static_cast<uint32_t>(p.O) - b);
+    if (gpc == 0) return span(b, n);
+    // (the last chunk may be short: G divides O, and what is left of it)
+    return Span{static_cast<uint32_t>(ch) * static_cast<uint32_t>(gpc),
+                n == BK ? span0.nrows : static_cast<int>(n / static_cast<uint32_t>(p.G)) * p.K, 0};
   };
-  auto scatter = [&](uint8_t* wt, const Span& s, int v, int group, const Unit<T>& val, const u32x2_t& ix) __attribute__((always_inline)) {
-    const int r = v / (MODE == kBack ? UC : UPR), u = v % (MODE == kBack ? UC : UPR);
-    if (r >= s.nrows) return;
-    const int row0 = s.first + group * p.G;
+  // element offset of a unit from its span's first packed row (a unit without one reads the last and is not written)
+  auto unit_off = [&](const Span& s, int v) __attribute__((always_inline)) {
+    const uint32_t r = static_cast<uint32_t>(max(min(v / kUnitsOfRow, s.nrows - 1), 0));
+    return r * static_cast<uint32_t>(p.C) + 8u * static_cast<uint32_t>(v % kUnitsOfRow);
+  };
+  auto load_unit = [&](const Span& s, int ch, int v, Unit<T>& val, u32x2_t& ix) __attribute__((always_inline)) {
+    const int64_t c0 = kFwd ? static_cast<int64_t>(ch) * BK : w0 + w * TQ;
+    const int64_t at = static_cast<int64_t>(s.g_lo) * p.K * p.C + c0;
+    const uint32_t off = unit_off(s, v);
+    const T* vb = vals + at;
+    const uint8_t* ib = idx + at;
+    if (c0 + (kFwd ? BK : TQ) <= p.C) {
+      load_full<8>(val, reinterpret_cast<const T*>(reinterpret_cast<const char*>(vb) + off * static_cast<uint32_t>(sizeof(T))));
+      load_full<8>(ix, ib + off);
+    } else {
+      const int64_t left = p.C - c0 - 8 * (v % kUnitsOfRow);
+      load_tail<8>(val, vb + off, left);
+      load_tail<8>(ix, ib + off, left);
+    }
+  };
+  uint8_t* trash = lds + TEAMS * 2 * kBuf;
+  // Whole groups lie in the wave's rows (gated, plain) or in a chunk (back) and
+  // G is a power of two: no entry has to be checked, and its place is its
+  // group's first plus idx rows, or plus idx elements of a row.
+  const bool fit = (p.G & (p.G - 1)) == 0 && p.G <= (kFwd ? TQ : BK);
+  const uint32_t gmask = static_cast<uint32_t>(p.G - 1) * 0x01010101u;  // (an index past its group stays in the tile)
+  // Order of a unit's entries (bf16): back, the rows of the packing over the
+  // 16-byte slots of a column block; else the units of a row over a slot's words.
+  const Shuffle sh = make_shuffle(sizeof(T) != 2 ? 0u
+                                  : kFwd         ? 2u * (static_cast<uint32_t>(lane) & 3u)
+                                                 : static_cast<uint32_t>(lane / kUnitsOfRow) & 7u);
+  uint32_t eoff[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int t = row0 + static_cast<int>((ix[e >> 2] >> (8 * (e & 3))) & 0xffu);
-      if (t >= 0 && t < lim) {
-        const uint32_t at = kFwd ? elem_addr<T>(static_cast<uint32_t>(w * TQ + t), static_cast<uint32_t>(8 * u + e))
-                                 : elem_addr<T>(static_cast<uint32_t>(w * TQ + 8 * u + e), static_cast<uint32_t>(t));
-        if constexpr (sizeof(T) == 2)
-          *reinterpret_cast<uint16_t*>(wt + at) = static_cast<uint16_t>(val.d[0][e >> 1] >> (16 * (e & 1)));
-        else
-          *reinterpret_cast<uint32_t*>(wt + at) = val.d[e >> 2][e & 3];
+  for (int e = 0; e < 8; ++e) eoff[e] = kFwd ? ecol<T>(static_cast<uint32_t>(e) ^ sh.m) : 16u * (static_cast<uint32_t>(e) ^ sh.m);
+  auto put = [&](uint8_t* to, const Unit<T>& val, int e) __attribute__((always_inline)) {
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(val.d[0][e >> 1] >> (16 * (e & 1)));
+    else
+      *reinterpret_cast<uint32_t*>(to) = val.d[e >> 2][e & 3];
+  };
+  auto scatter = [&](uint8_t* wt, const Span& s, int v, int row_of_group, Unit<T>& val, u32x2_t& ix) __attribute__((always_inline)) {
+    const uint32_t u = static_cast<uint32_t>(v % kUnitsOfRow);
+    if constexpr (sizeof(T) == 2) shuffle(sh, val, ix);
+    const uint32_t row0 = static_cast<uint32_t>(s.first + row_of_group);  // the group's first row / element
+    const bool there = v / kUnitsOfRow < s.nrows;
+    const uint32_t r0 = static_cast<uint32_t>(w * TQ);
+    if (fit) {
+      if (!there) return;
+      uint8_t* at = wt + (kFwd ? erow(r0 + row0) + ecol<T>(8 * u) : erow(r0 + 8 * u) + ecol<T>(row0));
+      const u32x2_t im = {ix[0] & gmask, ix[1] & gmask};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t i = (im[e >> 2] >> (8 * (e & 3))) & 0xffu;
+        const uint32_t step = kFwd ? (TQ > 16 ? erow(i) : i << 4) : ecol<T>(i);
+        put(at + step + eoff[e], val, e);
+      }
+    } else {
+      const uint32_t most = there ? lim : 0u;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t t = row0 + ((ix[e >> 2] >> (8 * (e & 3))) & 0xffu);
+        const uint32_t at = (kFwd ? erow(r0 + t) + ecol<T>(8 * u) : erow(r0 + 8 * u) + ecol<T>(t)) + eoff[e];
+        put(t < most ? wt + at : trash, val, e);
       }
     }
   };
-  auto load_w = [&](int ch) __attribute__((always_inline)) {
+  auto load_w = [&](int ch, int set) __attribute__((always_inline)) {
     if constexpr (MODE != kGrad && PL > 0) {
-      const Span s = kFwd ? gspan : span(ch);
+      const Span s = span_of(ch);
 #pragma unroll
-      for (int i = 0; i < PL; ++i) load_unit(s, ch, lane + 64 * i, pv[i], pi[i]);
+      for (int i = 0; i < PL; ++i) load_unit(s, ch, lane + 64 * i, pv[set][i], pi[set][i]);
     }
   };
-  auto store_w = [&](uint8_t* wt, int ch) __attribute__((always_inline)) {
+  auto store_w = [&](uint8_t* wt, int ch, int set) __attribute__((always_inline)) {
     if constexpr (MODE != kGrad) {
 #pragma unroll
       for (int i = 0; i < TQ / 8; ++i)
         *reinterpret_cast<u32x4_t*>(wt + w * TQ * kRowBytes + (i * 64 + lane) * 16) = u32x4_t{0u, 0u, 0u, 0u};
       asm volatile("" ::: "memory");  // the zeros come first; one wave's LDS writes stay in order
-      const Span s = kFwd ? gspan : span(ch);
+      const Span s = span_of(ch);
       if constexpr (PL > 0) {
 #pragma unroll
-        for (int i = 0; i < PL; ++i) scatter(wt, s, lane + 64 * i, gl[i], pv[i], pi[i]);
+        for (int i = 0; i < PL; ++i) scatter(wt, s, lane + 64 * i, grow[i], pv[set][i], pi[set][i]);
       } else {
-        const int units = s.nrows * (MODE == kBack ? UC : UPR);
+        const int units = s.nrows * kUnitsOfRow;
 #pragma unroll 1
         for (int v = lane; v < units; v += 64) {
-          load_unit(s, ch, v, pv[0], pi[0]);
-          scatter(wt, s, v, v / (MODE == kBack ? UC : UPR) / p.K, pv[0], pi[0]);
+          load_unit(s, ch, v, pv[0][0], pi[0][0]);
+          scatter(wt, s, v, v / kUnitsOfRow / p.K * p.G, pv[0][0], pi[0][0]);
         }
       }
     }
   };
 
-  auto load_chunk = [&](int ch) __attribute__((always_inline)) {
+  auto load_chunk = [&](int ch, int set) __attribute__((always_inline)) {
     if constexpr (MODE == kGrad) {
-      load_quads(qy, dY, p.O, w0, TW, ch);
-      load_quads(qx, X, p.C, n0, TN, ch);
+      load_quads(qy[set], dY, p.O, w0, TW, ch);
+      load_quads(qx[set], X, p.C, n0, TN, ch);
     } else {
-      load_x(ch);
-      load_w(ch);
+      load_x(ch, set);
+      load_w(ch, set);
     }
   };
-  auto store_chunk = [&](uint8_t* buf, int ch) __attribute__((always_inline)) {
+  auto store_chunk = [&](uint8_t* buf, int ch, int set) __attribute__((always_inline)) {
     if constexpr (MODE == kGrad) {
-      store_quads(buf + kXTile, qy, TW);
-      store_quads(buf, qx, TN);
+      store_quads(buf + kXTile, qy[set], TW);
+      store_quads(buf, qx[set], TN);
     } else {
-      store_x(buf);
-      store_w(buf + kXTile, ch);
+      store_x(buf, set);
+      store_w(buf + kXTile, ch, set);
     }
   };
 
@@ -286,34 +386,46 @@ __global__ __launch_bounds__(TEAMS * kThreads, TEAMS > 2 ? TEAMS : 2) void tile_
   // the team's chunks are team, team + TEAMS, ...; every team makes the same number of rounds (barriers)
   const int rounds = (nch + TEAMS - 1) / TEAMS;
   const auto chunk = [&](int i) { return team + TEAMS * i; };
+#pragma unroll
+  for (int i = 0; i < ND; ++i)
+    if (chunk(i) < nch) load_chunk(chunk(i), i);
   if (chunk(0) < nch) {
-    load_chunk(chunk(0));
-    store_chunk(bufs, chunk(0));
-    if (chunk(1) < nch) load_chunk(chunk(1));
+    store_chunk(bufs, chunk(0), 0);
+    if (chunk(ND) < nch) load_chunk(chunk(ND), 0);
   }
-#pragma unroll 1
-  for (int i = 0; i < rounds; ++i) {
-    // round i's chunk is complete in its buffer, and nobody reads the one of round i - 1 any more
+  // Round i: its chunk is complete in its buffer, and nobody reads the one of
+  // round i - 1 any more, which takes chunk i + 1 out of its registers (set
+  // `next`), which take chunk i + 1 + ND.
+  auto round = [&](int i, int next) __attribute__((always_inline)) {
     lds_barrier();
     const uint8_t* cur = bufs + (i & 1) * kBuf;
     if (chunk(i + 1) < nch) {
-      store_chunk(bufs + ((i + 1) & 1) * kBuf, chunk(i + 1));
-      if (chunk(i + 2) < nch) load_chunk(chunk(i + 2));
+      store_chunk(bufs + ((i + 1) & 1) * kBuf, chunk(i + 1), next);
+      if (chunk(i + 1 + ND) < nch) load_chunk(chunk(i + 1 + ND), next);
     }
-    if (chunk(i) >= nch) continue;
+    if (chunk(i) >= nch) return;
     const uint8_t* xt = cur;
     const uint8_t* wt = cur + kXTile;
 #pragma unroll
     for (int ks = 0; ks < UPR / 4; ++ks) {
       Unit<T> a[OT], b[NT];
 #pragma unroll
-      for (int o = 0; o < OT; ++o) a[o] = read_unit<T>(wt, static_cast<uint32_t>(wo * (TW / 2) + 16 * o) + li, 4u * ks + lq);
+      for (int o = 0; o < OT; ++o) a[o] = MODE == kGrad
+                   ? read_unit<T>(wt, static_cast<uint32_t>(wo * (TW / 2) + 16 * o) + li, 4u * ks + lq)
+                   : read_expanded<T>(wt, static_cast<uint32_t>(wo * (TW / 32) + o), 4u * ks + lq, li);
 #pragma unroll
       for (int n = 0; n < NT; ++n) b[n] = read_unit<T>(xt, static_cast<uint32_t>(wn * (TN / 2) + 16 * n) + li, 4u * ks + lq);
 #pragma unroll
       for (int o = 0; o < OT; ++o)
 #pragma unroll
         for (int n = 0; n < NT; ++n) mma(acc[o][n], a[o], b[n]);
+    }
+  };
+#pragma unroll 1
+  for (int i = 0; i < rounds; i += ND) {
+    round(i, ND - 1);
+    if constexpr (ND == 2) {
+      if (i + 1 < rounds) round(i + 1, 0);
     }
   }
 
@@ -450,7 +562,7 @@ hipError_t launch(const TParams& q, hipStream_t s) {
   TParams p = q;
   constexpr int kOperands = TEAMS * 2 * (TN + TW) * kRowBytes;
   constexpr int kPark = MODE == kGrad ? TN * (TW + 4) * 4 : 0;
-  constexpr int kLds = kOperands > kPark ? kOperands : kPark;
+  constexpr int kLds = (kOperands > kPark ? kOperands : kPark) + 16;  // and the word for entries of other tiles
   const int64_t along_n = MODE == kGrad ? p.C : p.N;
   const int64_t along_w = MODE == kBack ? p.C : p.O;
   const int64_t nnb = (along_n + TN - 1) / TN, nwb = (along_w + TW - 1) / TW;

@@ -6,6 +6,6 @@
 namespace cci {
 
 bool wide_back_supports(const BlockProduct& a) { return supports<kWBack>(a); }
-hipError_t launch_wide_back(const BlockProduct& a, hipStream_t s) { return launch_wide<kWBack>(a, s); }
+hipError_t launch_wide_back(const BlockProduct& a, int pt, hipStream_t s) { return launch_wide<kWBack>(a, pt, s); }
 
 }  // namespace cci

@@ -6,6 +6,6 @@
 namespace cci {
 
 bool wide_gated_supports(const BlockProduct& a) { return supports<kWGated>(a); }
-hipError_t launch_wide_gated(const BlockProduct& a, hipStream_t s) { return launch_wide<kWGated>(a, s); }
+hipError_t launch_wide_gated(const BlockProduct& a, int pt, hipStream_t s) { return launch_wide<kWGated>(a, pt, s); }
 
 }  // namespace cci
