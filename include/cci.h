@@ -431,7 +431,8 @@ cci_status cci_layernorm(const void *X, cci_dtype t, int64_t N, int64_t C,
                          void *Y, float *mean, float *rstd, void *stream);
 
 /* Bytes of the workspace of cci_layernorm_bwd: the partial sums of the weight
- * gradients (at most 256 x 2 x C fp32, more for C > 16384). */
+ * gradients (at most 256 x 2 x C fp32; 512 x 2 x C for C <= 1024; 2 N more for
+ * C > 16384). */
 cci_status cci_layernorm_bwd_workspace(int64_t N, int64_t C, size_t *bytes);
 
 /* Its backward pass: with xh = (x - mean) * rstd and q = dY * gamma,

@@ -460,28 +460,28 @@ def spmm_bits(X: torch.Tensor, vals: torch.Tensor, idx: torch.Tensor, G: int, id
 
 # ------------------------------------------------------ feed-forward block --
 
-class _on:
-    """The device of a call's tensors made current for its launches (a launch
-    on another device's stream is an error); nothing to do when it is."""
-    __slots__ = ("dev", "back")
+_get_device = torch._C._cuda_getDevice
 
-    def __init__(self, dev):
-        self.dev, self.back = dev.index, -1
 
-    def __enter__(self):
-        if self.dev is not None and self.dev != torch.cuda.current_device():
-            self.back = torch.cuda.current_device()
-            torch.cuda.set_device(self.dev)
+def _enter(dev) -> int:
+    """Make the device of a call's tensors current for its launches (a launch on
+    another device's stream is an error): the device to go back to, or -1."""
+    cur = _get_device()
+    if dev.index == cur:
+        return -1
+    torch.cuda.set_device(dev)
+    return cur
 
-    def __exit__(self, *exc):
-        if self.back >= 0:
-            torch.cuda.set_device(self.back)
+
+def _leave(back: int):
+    if back >= 0:
+        torch.cuda.set_device(back)
 
 
 def _tensor(t, name, shape, dtype, device):
     """Check a contiguous input tensor of one shape, dtype and device."""
     _dev(t)
-    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device:
+    if t.shape != shape or t.dtype != dtype or t.device != device:
         raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
     return t
 
@@ -515,11 +515,14 @@ def layernorm(X: torch.Tensor, gamma=None, beta=None, eps: float = 1e-5, *, out=
         if v is not None:
             _tensor(v, name, (C,), torch.float32, dev)
     code = _code(X.dtype)
-    Y = _out(out, (N, C), X.dtype, dev)
+    Y = torch.empty_like(X) if out is None else _out(out, (N, C), X.dtype, dev)
     mean, rstd = torch.empty(N, dtype=torch.float32, device=dev), torch.empty(N, dtype=torch.float32, device=dev)
-    with _on(dev):
+    back = _enter(dev)
+    try:
         _check(_lib.cci_layernorm(_ptr(X), code, N, C, _ptr(gamma), _ptr(beta), eps, _ptr(Y), _ptr(mean), _ptr(rstd),
                                   _stream(X)))
+    finally:
+        _leave(back)
     return Y, mean, rstd
 
 
@@ -538,11 +541,14 @@ def layernorm_bwd(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor, rstd: t
     nb = _sz()
     _check(_lib.cci_layernorm_bwd_workspace(N, C, ctypes.byref(nb)))
     ws = torch.empty(nb.value, dtype=torch.uint8, device=dev)
-    dX = torch.empty((N, C), dtype=X.dtype, device=dev) if need_dx else None
+    dX = torch.empty_like(X) if need_dx else None
     dg, db = (torch.empty(C, dtype=torch.float32, device=dev) if need_dw else None for _ in range(2))
-    with _on(dev):
+    back = _enter(dev)
+    try:
         _check(_lib.cci_layernorm_bwd(_ptr(dY), _ptr(X), code, N, C, _ptr(gamma), _ptr(mean), _ptr(rstd), _ptr(dX),
                                       _ptr(dg), _ptr(db), _ptr(ws), nb.value, _stream(X)))
+    finally:
+        _leave(back)
     return dX, dg, db
 
 
@@ -558,11 +564,14 @@ def gated_spmm(X: torch.Tensor, vals: torch.Tensor, idx: torch.Tensor, G: int, *
         raise ValueError("the packing must hold 2 F rows with F a multiple of G")
     F = O // 2
     code = _code(X.dtype)
-    H = _out(out, (N, F), X.dtype, dev)
+    H = torch.empty(N, F, dtype=X.dtype, device=dev) if out is None else _out(out, (N, F), X.dtype, dev)
     pre = torch.empty((N, O), dtype=X.dtype, device=dev) if save_pre else None
-    with _on(dev):
+    back = _enter(dev)
+    try:
         _check(_lib.cci_gated_spmm(_ptr(X), code, N, C, _ptr(vals), _ptr(idx), F, G, K, ACTS[act], _ptr(H), _ptr(pre),
                                    _stream(X)))
+    finally:
+        _leave(back)
     return (H, pre) if save_pre else H
 
 
@@ -580,12 +589,15 @@ def gated_spmm_bwd(dH: torch.Tensor, pre: torch.Tensor, X: torch.Tensor, vals: t
     _tensor(dH, "dH", (N, F), X.dtype, dev), _tensor(pre, "pre", (N, O), X.dtype, dev)
     dv_t = dvals_dtype or X.dtype
     code, dv_code = _code(X.dtype), _code(dv_t)
-    dpre = torch.empty((N, O), dtype=X.dtype, device=dev)
-    dX = torch.empty((N, C), dtype=X.dtype, device=dev) if need_dx else None
+    dpre = torch.empty_like(pre)
+    dX = torch.empty_like(X) if need_dx else None
     dv = torch.empty(vals.shape, dtype=dv_t, device=dev) if need_dvals else None
-    with _on(dev):
+    back = _enter(dev)
+    try:
         _check(_lib.cci_gated_spmm_bwd(_ptr(dH), _ptr(pre), _ptr(X), code, N, C, _ptr(vals), _ptr(idx), F, G, K,
                                        ACTS[act], _ptr(dpre), _ptr(dX), _ptr(dv), dv_code, _stream(X)))
+    finally:
+        _leave(back)
     return dpre, dX, dv
 
 
@@ -597,9 +609,12 @@ def spmm_t(dY: torch.Tensor, vals: torch.Tensor, idx: torch.Tensor, G: int, *, o
     C = vals.shape[2]
     code = _code(dY.dtype)
     dX = _out(out, (N, C), out_dtype or dY.dtype, dev)
-    with _on(dev):
+    back = _enter(dev)
+    try:
         _check(_lib.cci_spmm_t(_ptr(dY), code, N, O, _ptr(vals), _ptr(idx), C, G, K, _ptr(dX), _code(dX.dtype),
                                _stream(dY)))
+    finally:
+        _leave(back)
     return dX
 
 
@@ -628,7 +643,10 @@ def spmm_adapters(X: torch.Tensor, vals: torch.Tensor, idx: torch.Tensor, G: int
     _check(_lib.cci_spmm_adapters_workspace(N, C, O, L, R, ycode, ctypes.byref(nb)))
     ws = torch.empty(nb.value, dtype=torch.uint8, device=dev)
     ad = Adapters(_ptr(A), _ptr(B), _ptr(alpha), _ptr(rows), L, R)
-    with _on(dev):
+    back = _enter(dev)
+    try:
         _check(_lib.cci_spmm_adapters(_ptr(X), code, N, C, _ptr(vals), code, _ptr(idx), O, G, K, ctypes.byref(ad), ep,
                                       _ptr(Y), ycode, _ptr(ws), nb.value, _stream(X)))
+    finally:
+        _leave(back)
     return Y

@@ -4,20 +4,24 @@
 // projection then takes D as its residual, so the sum is rounded once more
 // than the projection alone (D, in the output's type, is a small part of it).
 //
-// Both kernels work on tiles of 16 rows and walk over the distinct adapters
-// among them: the matrix cores multiply all 16 rows by one adapter, and the
-// rows that have it keep the result.  A prompt's tile has one or two; a
-// decoding batch up to 16, whose weights have to be read in any case.
+// Both kernels work on tiles of 16 RT rows and walk over the distinct adapters
+// among them: the matrix cores multiply all rows by one adapter, and the rows
+// that have it keep the result.  A prompt's tile has one or two (RT = 4: the
+// adapter's fragments serve 64 rows); a decoding batch up to 16 in 16 rows,
+// whose weights have to be read in any case.
 //   shrink  T: a workgroup of four waves sums one of S column ranges of one
 //           tile, the waves taking turns at its 32-column steps, and adds the
 //           four partial tiles in LDS.  With few tiles P workgroups share the
 //           distinct adapters of one.  The S partial sums stay apart (fp32):
 //           no atomics, equal calls give equal bits.
-//   expand  a wave adds them up in order and multiplies by 64 rows of B.  With
-//           bf16 operands T enters as the sum of two bf16 values (16 bits of
-//           mantissa): it is not rounded to one.
-// Adapter weights bind while decoding, X (shrink) and D (expand) for prompts.
+//   expand  the workgroup adds them up in order into LDS, and a wave multiplies
+//           by 64 rows of B.  With bf16 operands T enters as the sum of two
+//           bf16 values (16 bits of mantissa): it is not rounded to one.
+// Fragments read from rows of memory cost the L1 one access per lane and 16
+// bytes; that and the latency of a chain of loads bind (3001 rows, C = O =
+// 4096, R = 32: FIGURES).
 #include <algorithm>
+#include <type_traits>
 
 #include "cci_block.hpp"
 #include "cci_frag.hpp"
@@ -26,9 +30,8 @@ namespace cci {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
-constexpr int kRows = 16;       // rows of a tile
-constexpr int kRankBlocks = 4;  // blocks of 16 ranks a shrink pass accumulates
 constexpr int kOutBlocks = 4;   // blocks of 16 outputs of an expand wave
+constexpr int kOutTile = kWaves * 16 * kOutBlocks;  // outputs of its workgroup's block
 
 struct APlan {
   int32_t S, P;      // column ranges, workgroups sharing a tile's adapters
@@ -49,66 +52,154 @@ struct AParams {
   int32_t R, S, P, d_f32;
 };
 
-// The adapter of row n of the tile (-1: none), for lane n % 16.
+// The adapter of row n (-1: none).
 __device__ __forceinline__ int32_t row_adapter(const AParams& p, int64_t n) {
   if (n >= p.N) return -1;
   const int32_t a = global_ptr<const int32_t>(p.rows)[n];
   return a >= 0 && a < p.L ? a : -1;
 }
 
-template <typename T>
+// The distinct adapters of a tile's rows in turn: lane l has row l of the tile
+// (lanes past the rows have none), and `todo` its rows still to do.
+struct Walk {
+  int32_t mine;
+  uint64_t todo;
+};
+template <int RT>
+__device__ __forceinline__ Walk start_walk(const AParams& p, int64_t n0, int lane) {
+  const int32_t a = lane < 16 * RT ? row_adapter(p, n0 + lane) : -1;
+  return Walk{a, __ballot(a >= 0)};
+}
+__device__ __forceinline__ int32_t next_adapter(Walk& k) {
+  const int32_t a = __builtin_amdgcn_readfirstlane(__shfl(k.mine, __builtin_ctzll(k.todo)));
+  k.todo &= ~__ballot(k.mine == a);
+  return a;
+}
+
+// KB: blocks of 16 ranks of a pass.
+template <typename T, int RT, int KB>
 __global__ __launch_bounds__(kThreads) void shrink_kernel(AParams p) {
-  __shared__ f32x4_t red[kWaves][kRankBlocks][64];
+  __shared__ f32x4_t red[kWaves][KB][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const uint32_t li = lane & 15, lq = lane >> 4;
   const uint32_t per = static_cast<uint32_t>(p.S) * static_cast<uint32_t>(p.P);
   const uint32_t tile = blockIdx.x / per, rest = blockIdx.x - tile * per;
   const int32_t sl = static_cast<int32_t>(rest / p.P), turn = static_cast<int32_t>(rest % p.P);
-  const int64_t n = static_cast<int64_t>(tile) * kRows + li;
+  const int64_t n0 = static_cast<int64_t>(tile) * (16 * RT);
   const int64_t c_lo = sl * p.cols, c_hi = min(p.C, c_lo + p.cols);
-  const T* x = global_ptr<const T>(p.X) + min(n, p.N - 1) * p.C;  // (rows past the last have no adapter)
+  const T* X = global_ptr<const T>(p.X);
   const T* A = global_ptr<const T>(p.A);
   float* part = global_ptr<float>(p.part);
-  const int32_t mine = row_adapter(p, n);
+  const T* x[RT];  // (rows past the last have no adapter)
+  int32_t mine[RT];
+#pragma unroll
+  for (int t = 0; t < RT; ++t) {
+    const int64_t n = n0 + 16 * t + li;
+    x[t] = X + min(n, p.N - 1) * p.C;
+    mine[t] = row_adapter(p, n);
+  }
   const int rank_blocks = (p.R + 15) / 16;
-  uint64_t todo = __ballot(mine >= 0) & 0xffffu;  // rows (lanes 0 .. 15) still to do
-  for (int32_t ord = 0; todo; ++ord) {
-    const int32_t a = __builtin_amdgcn_readfirstlane(__shfl(mine, __builtin_ctzll(todo)));
-    todo &= ~__ballot(mine == a);
+  Walk walk = start_walk<RT>(p, n0, lane);
+  for (int32_t ord = 0; walk.todo; ++ord) {
+    const int32_t a = next_adapter(walk);
     if (ord % p.P != turn) continue;
-    for (int rb0 = 0; rb0 < rank_blocks; rb0 += kRankBlocks) {
-      f32x4_t acc[kRankBlocks];
+    for (int rb0 = 0; rb0 < rank_blocks; rb0 += KB) {
+      f32x4_t acc[KB][RT];
 #pragma unroll
-      for (int b = 0; b < kRankBlocks; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      const int nb = min(kRankBlocks, rank_blocks - rb0);
-      const int64_t r0 = 16 * rb0 + li;
-      const T* ar = A + static_cast<int64_t>(a) * p.R * p.C;
-      for (int64_t c0 = c_lo + 32 * w; c0 < c_hi; c0 += 32 * kWaves) {
-        const int64_t c = c0 + 8 * lq, left = p.C - c;
-        const bool whole = c0 + 32 <= p.C;
-        Unit<T> xf, af[kRankBlocks];
-        load_part<8>(xf, x + c, left, whole);
+      for (int b = 0; b < KB; ++b)
 #pragma unroll
-        for (int b = 0; b < kRankBlocks; ++b)  // (ranks past the last read it again: their sums are not stored)
-          if (b < nb) load_part<8>(af[b], ar + min(r0 + 16 * b, static_cast<int64_t>(p.R - 1)) * p.C + c, left, whole);
+        for (int t = 0; t < RT; ++t) acc[b][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      const int nb = min(KB, rank_blocks - rb0);
+      const T* ar[KB];  // (ranks past the last read it again: their sums are not stored)
 #pragma unroll
-        for (int b = 0; b < kRankBlocks; ++b)
-          if (b < nb) mma(acc[b], af[b], xf);
+      for (int b = 0; b < KB; ++b)
+        ar[b] = A + (static_cast<int64_t>(a) * p.R + min(16 * (rb0 + b) + static_cast<int>(li), p.R - 1)) * p.C;
+      // Steps of 32 columns, two at a time; the loads of whole ones have no
+      // branch, so that all of them are in flight.
+      struct Step {
+        Unit<T> x[RT], a[KB];
+      };
+      auto load = [&](Step& q, int64_t c, auto tail) __attribute__((always_inline)) {
+        constexpr bool kWhole = !decltype(tail)::value;
+#pragma unroll
+        for (int t = 0; t < RT; ++t) load_part<8>(q.x[t], x[t] + c, p.C - c, kWhole);
+#pragma unroll
+        for (int b = 0; b < KB; ++b) load_part<8>(q.a[b], ar[b] + c, p.C - c, kWhole);
+      };
+      auto multiply = [&](const Step& q) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int t = 0; t < RT; ++t) mma(acc[b][t], q.a[b], q.x[t]);
+      };
+      const int64_t whole = min(c_hi, p.C / 32 * 32);
+      int64_t c0 = c_lo + 32 * w;
+      Step q0, q1;
+      for (; c0 + 32 * kWaves < whole; c0 += 64 * kWaves) {
+        load(q0, c0 + 8 * lq, std::false_type{});
+        load(q1, c0 + 32 * kWaves + 8 * lq, std::false_type{});
+        multiply(q0);
+        multiply(q1);
       }
-      __syncthreads();  // the previous pass's sums are read
+      if (c0 < whole) {
+        load(q0, c0 + 8 * lq, std::false_type{});
+        multiply(q0);
+        c0 += 32 * kWaves;
+      }
+      if (c0 < c_hi) {
+        load(q0, c0 + 8 * lq, std::true_type{});
+        multiply(q0);
+      }
 #pragma unroll
-      for (int b = 0; b < kRankBlocks; ++b)
-        if (b < nb) red[w][b][lane] = acc[b];
-      __syncthreads();
-      // wave w finishes block w: lane (li, lq) holds ranks 16 (rb0 + w) + 4 lq .. +3 of row li
-      if (w < nb && mine == a) {
-        const f32x4_t t = red[0][w][lane] + red[1][w][lane] + red[2][w][lane] + red[3][w][lane];
-        const int64_t r = 16 * (rb0 + w) + 4 * lq;
-        const float v[4] = {t[0], t[1], t[2], t[3]};
-        store4<float>(part + (static_cast<int64_t>(sl) * p.N + n) * p.R + r, v, p.R - r, p.R % 4 == 0);
+      for (int t = 0; t < RT; ++t) {
+        __syncthreads();  // the previous sums are read
+#pragma unroll
+        for (int b = 0; b < KB; ++b) red[w][b][lane] = acc[b][t];
+        __syncthreads();
+        // wave w finishes block w: lane (li, lq) holds ranks 16 (rb0 + w) + 4 lq .. +3 of row li
+        if (w < nb && mine[t] == a) {
+          const f32x4_t s = red[0][w][lane] + red[1][w][lane] + red[2][w][lane] + red[3][w][lane];
+          const int64_t n = n0 + 16 * t + li, r = 16 * (rb0 + w) + 4 * lq;
+          const float v[4] = {s[0], s[1], s[2], s[3]};
+          store4<float>(part + (static_cast<int64_t>(sl) * p.N + n) * p.R + r, v, p.R - r, p.R % 4 == 0);
+        }
       }
     }
   }
+}
+
+// The workgroup's sum of the column ranges' parts of `rows` rows from n0, times
+// alpha, into t[row][pitch] (padded: R rounded up to 8; rows without an
+// adapter and ranks past the last are 0).  A thread takes 4 ranks; the loads of
+// four ranges are in flight together and added in the ranges' order.
+__device__ __forceinline__ void sum_parts(const AParams& p, int64_t n0, int rows, int32_t padded, int32_t pitch, float* t) {
+  const float* part = global_ptr<const float>(p.part);
+  const int64_t next = p.N * p.R;  // from a range's part to the next
+  const int32_t quads = padded / 4;
+  for (int32_t i = threadIdx.x; i < rows * quads; i += kThreads) {
+    const int32_t row = i / quads, r = 4 * (i - row * quads);
+    const int64_t n = min(n0 + row, p.N - 1);
+    const int32_t a = row_adapter(p, n0 + row);
+    const float* q = part + n * p.R + r;  // (a row without an adapter has no parts: what is read there is not used)
+    f32x4_t sum{0.f, 0.f, 0.f, 0.f};
+    int32_t k = 0;
+    for (; k + 4 <= p.S; k += 4) {
+      f32x4_t v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) load_elems<4>(v[j], q + (k + j) * next, p.R - r);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum += v[j];
+    }
+    for (; k < p.S; ++k) {
+      f32x4_t v;
+      load_elems<4>(v, q + k * next, p.R - r);
+      sum += v;
+    }
+    if (p.alpha) sum *= global_ptr<const float>(p.alpha)[a >= 0 ? a : 0];
+    if (a < 0) sum = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    *reinterpret_cast<f32x4_t*>(t + row * pitch + r) = sum;
+  }
+  __syncthreads();
 }
 
 // T as MFMA operands: fp32 as it is, bf16 as high part + low part.
@@ -119,98 +210,124 @@ __device__ __forceinline__ Split split(const float (&t)[8]) {
   Split s;
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
-    uint32_t hi[2], lo[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      hi[i] = f32_to_bf16_rne(t[e + i]);
-      const float d = t[e + i] - bf16_to_f32(static_cast<uint16_t>(hi[i]));
-      lo[i] = __builtin_isfinite(d) ? f32_to_bf16_rne(d) : 0u;  // (an infinite T stays infinite)
-    }
-    s.hi.d[0][e >> 1] = hi[0] | (hi[1] << 16);
-    s.lo.d[0][e >> 1] = lo[0] | (lo[1] << 16);
+    const uint32_t hi = pack_bf16(t[e], t[e + 1]);
+    const float d0 = t[e] - __uint_as_float(hi << 16), d1 = t[e + 1] - __uint_as_float(hi & 0xffff0000u);
+    s.hi.d[0][e >> 1] = hi;
+    // (an infinite T stays infinite)
+    s.lo.d[0][e >> 1] = pack_bf16(__builtin_isfinite(d0) ? d0 : 0.0f, __builtin_isfinite(d1) ? d1 : 0.0f);
   }
   return s;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void expand_kernel(AParams p, uint32_t nob) {
+// A workgroup has 16 RT rows and every `groups`-th block of 256 outputs.
+template <typename T, int RT>
+__global__ __launch_bounds__(kThreads) void expand_kernel(AParams p, uint32_t nob, uint32_t groups) {
+  extern __shared__ __attribute__((aligned(16))) float tsum[];  // [16 RT][pitch]
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const uint32_t li = lane & 15, lq = lane >> 4;
-  const uint32_t tile = blockIdx.x / nob, ob = blockIdx.x - tile * nob;
-  const int64_t n = static_cast<int64_t>(tile) * kRows + li;
-  const int64_t o0 = (static_cast<int64_t>(ob) * kWaves + w) * (16 * kOutBlocks);
+  const uint32_t tile = blockIdx.x / groups;
+  const int64_t n0 = static_cast<int64_t>(tile) * (16 * RT);
   const T* B = global_ptr<const T>(p.B);
-  const float* part = global_ptr<const float>(p.part);
-  const int32_t mine = row_adapter(p, n);
-  f32x4_t out[kOutBlocks];
+  const int32_t padded = (p.R + 7) & ~7, pitch = padded + 4;  // (16 rows' units in different banks)
+  const Walk all = start_walk<RT>(p, n0, lane);
+  int32_t mine[RT];
 #pragma unroll
-  for (int b = 0; b < kOutBlocks; ++b) out[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  uint64_t todo = __ballot(mine >= 0) & 0xffffu;
-  if (o0 >= p.O) return;
-  while (todo) {
-    const int32_t a = __builtin_amdgcn_readfirstlane(__shfl(mine, __builtin_ctzll(todo)));
-    todo &= ~__ballot(mine == a);
-    const float s = p.alpha ? global_ptr<const float>(p.alpha)[a] : 1.0f;
-    f32x4_t acc[kOutBlocks];
-#pragma unroll
-    for (int b = 0; b < kOutBlocks; ++b) acc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int32_t rs = 0; rs < p.R; rs += 32) {
-      const int32_t r0 = rs + 8 * static_cast<int32_t>(lq);
-      // ranks r0 .. r0 + 7 of row li, the column ranges' sums added in order
-      float t[8] = {};
-      if (mine == a) {
-        for (int32_t k = 0; k < p.S; ++k) {
-          Unit<float> u;
-          load_elems<8>(u, part + (static_cast<int64_t>(k) * p.N + n) * p.R + r0, p.R - r0);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) t[e] += __uint_as_float(u.d[e >> 2][e & 3]);
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) t[e] *= s;
-      }
-      Unit<T> bf[kOutBlocks];
+  for (int t = 0; t < RT; ++t) mine[t] = row_adapter(p, n0 + 16 * t + li);
+  const bool vec = p.O % 4 == 0;
+  bool summed = false;
+  for (uint32_t ob = blockIdx.x - tile * groups; ob < nob; ob += groups) {
+    const int64_t o0 = (static_cast<int64_t>(ob) * kWaves + w) * (16 * kOutBlocks);
+    const auto load_b = [&](Unit<T> (&bf)[kOutBlocks], int32_t a, int32_t r0) __attribute__((always_inline)) {
 #pragma unroll
       for (int b = 0; b < kOutBlocks; ++b) {
         const int64_t o = min(o0 + 16 * b + li, p.O - 1);  // (outputs past the last are not stored)
         load_elems<8>(bf[b], B + (static_cast<int64_t>(a) * p.O + o) * p.R + r0, p.R - r0);
       }
-      if constexpr (sizeof(T) == 2) {
-        const Split q = split(t);
-#pragma unroll
-        for (int b = 0; b < kOutBlocks; ++b) {
-          mma(acc[b], bf[b], q.lo);
-          mma(acc[b], bf[b], q.hi);
-        }
-      } else {
-        Unit<float> q;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) q.d[e >> 2][e & 3] = __float_as_uint(t[e]);
-#pragma unroll
-        for (int b = 0; b < kOutBlocks; ++b) mma(acc[b], bf[b], q);
-      }
+    };
+    Walk walk = all;
+    Unit<T> bf[kOutBlocks];
+    int32_t a = -1;
+    if (walk.todo) {  // B of the first adapter, before the wait for the sums
+      a = next_adapter(walk);
+      load_b(bf, a, 8 * static_cast<int32_t>(lq));
     }
+    if (!summed) sum_parts(p, n0, 16 * RT, padded, pitch, tsum);
+    summed = true;
+    f32x4_t out[kOutBlocks][RT];
 #pragma unroll
     for (int b = 0; b < kOutBlocks; ++b)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) out[b][r] = mine == a ? acc[b][r] : out[b][r];
-  }
-  if (n >= p.N) return;
-  const bool vec = p.O % 4 == 0;
+      for (int t = 0; t < RT; ++t) out[b][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    while (a >= 0) {
+      f32x4_t acc[kOutBlocks][RT];
 #pragma unroll
-  for (int b = 0; b < kOutBlocks; ++b) {
-    const int64_t o = o0 + 16 * b + 4 * lq, at = n * p.O + o;
-    float v[4];
+      for (int b = 0; b < kOutBlocks; ++b)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      v[r] = out[b][r];
-      if (p.residual && o + r < p.O)
-        v[r] += p.d_f32 ? global_ptr<const float>(p.residual)[at + r]
-                        : bf16_to_f32(global_ptr<const uint16_t>(p.residual)[at + r]);
+        for (int t = 0; t < RT; ++t) acc[b][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int32_t rs = 0; rs < p.R; rs += 32) {
+        const int32_t r0 = rs + 8 * static_cast<int32_t>(lq);
+        if (rs > 0) load_b(bf, a, r0);
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+          // ranks r0 .. r0 + 7 of row li; a row of another adapter enters as 0 and is not kept
+          const f32x4_t* q = reinterpret_cast<const f32x4_t*>(tsum + (16 * t + li) * pitch + min(r0, padded - 8));
+          const f32x4_t q0 = q[0], q1 = q[1];
+          const bool keep = r0 < p.R && mine[t] == a;
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            v[e] = keep ? q0[e] : 0.0f;
+            v[4 + e] = keep ? q1[e] : 0.0f;
+          }
+          if constexpr (sizeof(T) == 2) {
+            const Split q = split(v);
+#pragma unroll
+            for (int b = 0; b < kOutBlocks; ++b) {
+              mma(acc[b][t], bf[b], q.lo);
+              mma(acc[b][t], bf[b], q.hi);
+            }
+          } else {
+            Unit<float> q;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q.d[e >> 2][e & 3] = __float_as_uint(v[e]);
+#pragma unroll
+            for (int b = 0; b < kOutBlocks; ++b) mma(acc[b][t], bf[b], q);
+          }
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < kOutBlocks; ++b)
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) out[b][t][r] = mine[t] == a ? acc[b][t][r] : out[b][t][r];
+      a = -1;
+      if (walk.todo) {
+        a = next_adapter(walk);
+        load_b(bf, a, 8 * static_cast<int32_t>(lq));
+      }
     }
-    if (p.d_f32)
-      store4<float>(global_ptr<float>(p.D) + at, v, p.O - o, vec);
-    else
-      store4<bf16_t>(global_ptr<bf16_t>(p.D) + at, v, p.O - o, vec);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+      const int64_t n = n0 + 16 * t + li;
+      if (n >= p.N) continue;
+#pragma unroll
+      for (int b = 0; b < kOutBlocks; ++b) {
+        const int64_t o = o0 + 16 * b + 4 * lq, at = n * p.O + o;
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          v[r] = out[b][t][r];
+          if (p.residual && o + r < p.O)
+            v[r] += p.d_f32 ? global_ptr<const float>(p.residual)[at + r]
+                            : bf16_to_f32(global_ptr<const uint16_t>(p.residual)[at + r]);
+        }
+        if (p.d_f32)
+          store4<float>(global_ptr<float>(p.D) + at, v, p.O - o, vec);
+        else
+          store4<bf16_t>(global_ptr<bf16_t>(p.D) + at, v, p.O - o, vec);
+      }
+    }
   }
 }
 
@@ -227,16 +344,8 @@ __global__ __launch_bounds__(kThreads) void expand_rows_kernel(AParams p, uint32
   const int32_t a = __builtin_amdgcn_readfirstlane(row_adapter(p, n));
   float v = 0.0f;
   if (a >= 0) {
-    const float* part = global_ptr<const float>(p.part);
-    const float s = p.alpha ? global_ptr<const float>(p.alpha)[a] : 1.0f;
     const int32_t padded = (p.R + 7) & ~7;
-    for (int32_t r = threadIdx.x; r < padded; r += kThreads) {
-      float sum = 0.0f;
-      if (r < p.R)
-        for (int32_t k = 0; k < p.S; ++k) sum += part[(static_cast<int64_t>(k) * p.N + n) * p.R + r];
-      t[r] = sum * s;
-    }
-    __syncthreads();
+    sum_parts(p, n, 1, padded, padded, t);
     if (o < p.O) {
       const T* b = global_ptr<const T>(p.B) + (static_cast<int64_t>(a) * p.O + o) * p.R;
       for (int32_t r = 0; r < p.R; r += 8) {
@@ -257,20 +366,57 @@ __global__ __launch_bounds__(kThreads) void expand_rows_kernel(AParams p, uint32
     global_ptr<uint16_t>(p.D)[at] = f32_to_bf16_rne(v);
 }
 
-constexpr int64_t kFewRows = 64;  // expand on the vector ALUs up to so many rows
+// Up to so many rows: tiles of 16 rows, and expand on the vector ALUs.
+constexpr int64_t kFewRows = 64;
 
-// About 512 workgroups: column ranges of at least 256 columns first, then,
-// for a decoding batch's few tiles, workgroups that share the adapters.
+// About 512 workgroups (64-row tiles: 256): column ranges of at least 256
+// columns first, then, for a decoding batch's few tiles, workgroups that share
+// the adapters.
 APlan plan(int64_t N, int64_t C, int64_t L) {
   APlan q{};
-  q.tiles = (N + kRows - 1) / kRows;
-  const int64_t want = std::max<int64_t>(1, 512 / std::max<int64_t>(q.tiles, 1));
+  const int64_t rows = N <= kFewRows ? 16 : 64;
+  q.tiles = (N + rows - 1) / rows;
+  const int64_t want = std::max<int64_t>(1, (N <= kFewRows ? 512 : 256) / std::max<int64_t>(q.tiles, 1));
   const int64_t S = std::min<int64_t>(std::min<int64_t>(want, 16), (C + 255) / 256);
   q.cols = (C + S - 1) / S;
   q.cols = (q.cols + 127) / 128 * 128;
   q.S = static_cast<int32_t>((C + q.cols - 1) / q.cols);
-  q.P = static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(16, std::min(L, N)), want * 2 / q.S)));
+  q.P = static_cast<int32_t>(
+      std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(rows, std::min(L, N)), want * 2 / q.S)));
   return q;
+}
+
+template <typename T>
+hipError_t launch_typed(const AdapterArgs& a, const APlan& q, const AParams& p, hipStream_t s) {
+  const int64_t shrink = q.tiles * q.S * q.P;
+  if (shrink > 0x7fffffff) return hipErrorInvalidConfiguration;
+  const dim3 grid(static_cast<uint32_t>(shrink)), block(kThreads);
+  const size_t row_bytes = static_cast<size_t>((a.R + 7) & ~7) * 4;
+  if (a.N <= kFewRows) {
+    const int64_t nob = (a.O + kThreads - 1) / kThreads;
+    if (nob > 0x7fffffff / a.N) return hipErrorInvalidConfiguration;
+    const auto kernel = a.R <= 16 ? shrink_kernel<T, 1, 1> : a.R <= 32 ? shrink_kernel<T, 1, 2> : shrink_kernel<T, 1, 4>;
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, p);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    hipLaunchKernelGGL((expand_rows_kernel<T>), dim3(static_cast<uint32_t>(a.N * nob)), block, row_bytes, s, p,
+                       static_cast<uint32_t>(nob));
+    return hipGetLastError();
+  }
+  const int64_t nob = (a.O + kOutTile - 1) / kOutTile;
+  const int64_t tiles32 = (a.N + 31) / 32;
+  if (nob > 0x7fffffff / tiles32) return hipErrorInvalidConfiguration;
+  const auto kernel = a.R <= 16 ? shrink_kernel<T, 4, 1> : shrink_kernel<T, 4, 2>;
+  hipLaunchKernelGGL(kernel, grid, block, 0, s, p);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  // tiles of 32 rows: their sums of up to 1024 ranks fit the LDS
+  static std::atomic<int8_t> lds_set[kMaxDevices];
+  const hipError_t e = set_lds_limit_once(lds_set, reinterpret_cast<const void*>(&expand_kernel<T, 2>), 32 * (1024 + 4) * 4);
+  if (e != hipSuccess) return e;
+  // one round of workgroups: each sums its rows' parts once for all of its blocks
+  const int64_t groups = std::max<int64_t>(1, std::min(nob, 512 / tiles32));
+  hipLaunchKernelGGL((expand_kernel<T, 2>), dim3(static_cast<uint32_t>(tiles32 * groups)), block, 32 * (row_bytes + 16), s, p,
+                     static_cast<uint32_t>(nob), static_cast<uint32_t>(groups));
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -297,31 +443,7 @@ hipError_t launch_adapters(const AdapterArgs& a, hipStream_t s) {
   p.S = q.S;
   p.P = q.P;
   p.d_f32 = a.d_t == DType::F32;
-  const int64_t g1 = q.tiles * q.S * q.P;
-  const int64_t nob = (a.O + kWaves * 16 * kOutBlocks - 1) / (kWaves * 16 * kOutBlocks);
-  if (g1 > 0x7fffffff || nob > 0x7fffffff || q.tiles > 0x7fffffff / nob) return hipErrorInvalidConfiguration;
-  const dim3 grid1(static_cast<uint32_t>(g1)), grid2(static_cast<uint32_t>(q.tiles * nob));
-  if (a.t == DType::F32)
-    hipLaunchKernelGGL((shrink_kernel<float>), grid1, dim3(kThreads), 0, s, p);
-  else
-    hipLaunchKernelGGL((shrink_kernel<bf16_t>), grid1, dim3(kThreads), 0, s, p);
-  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  if (a.N <= kFewRows) {
-    const int64_t blocks = (a.O + kThreads - 1) / kThreads;
-    if (blocks > 0x7fffffff / a.N) return hipErrorInvalidConfiguration;
-    const dim3 grid(static_cast<uint32_t>(a.N * blocks));
-    const size_t lds = static_cast<size_t>((a.R + 7) & ~7) * 4;
-    if (a.t == DType::F32)
-      hipLaunchKernelGGL((expand_rows_kernel<float>), grid, dim3(kThreads), lds, s, p, static_cast<uint32_t>(blocks));
-    else
-      hipLaunchKernelGGL((expand_rows_kernel<bf16_t>), grid, dim3(kThreads), lds, s, p, static_cast<uint32_t>(blocks));
-    return hipGetLastError();
-  }
-  if (a.t == DType::F32)
-    hipLaunchKernelGGL((expand_kernel<float>), grid2, dim3(kThreads), 0, s, p, static_cast<uint32_t>(nob));
-  else
-    hipLaunchKernelGGL((expand_kernel<bf16_t>), grid2, dim3(kThreads), 0, s, p, static_cast<uint32_t>(nob));
-  return hipGetLastError();
+  return a.t == DType::F32 ? launch_typed<float>(a, q, p, s) : launch_typed<bf16_t>(a, q, p, s);
 }
 
 }  // namespace cci

@@ -26,6 +26,14 @@ struct Unit {
   u32x4_t d[sizeof(T) / 2];
 };
 
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+// Two values as bf16, rounded to nearest even (v_cvt_pk_bf16_f32).
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{lo, hi}), bf16x2_t));
+}
+
 // Element e of a unit, in fp32.
 template <typename T>
 __device__ __forceinline__ float elem(const Unit<T>& u, int e) {
@@ -115,9 +123,7 @@ __device__ __forceinline__ void store4(YT* p, const float (&v)[4], int64_t left,
     if constexpr (std::is_same<YT, float>::value) {
       *reinterpret_cast<f32x4_t*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
     } else {
-      *reinterpret_cast<u32x2_t*>(p) =
-          u32x2_t{f32_to_bf16_rne(v[0]) | static_cast<uint32_t>(f32_to_bf16_rne(v[1])) << 16,
-                  f32_to_bf16_rne(v[2]) | static_cast<uint32_t>(f32_to_bf16_rne(v[3])) << 16};
+      *reinterpret_cast<u32x2_t*>(p) = u32x2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
     }
     return;
   }

@@ -13,6 +13,8 @@
 // over a workgroup's teams in LDS, and over the workgroups by a second kernel
 // in a fixed order (no atomics: equal calls give equal bits).
 // Rows too long for the registers are read again for every pass.
+#include <algorithm>
+
 #include "cci_block.hpp"
 #include "cci_frag.hpp"
 
@@ -21,7 +23,10 @@ namespace {
 
 constexpr int kCUs = 256;
 constexpr int kFwdThreads = 256;
-constexpr int kBwdThreads = 1024;
+// Threads of a backward workgroup: four teams, 1024 at most (more teams of short
+// rows would add up longer in LDS than they save in partial sums: 1537 x 1001
+// fp32 with sixteen 17 us).
+constexpr int bwd_threads(int tpr) { return tpr <= 256 ? 4 * tpr : 1024; }
 constexpr int kSumCols = 64, kSumGroups = 16;  // reduction of the partial weight gradients
 
 // 8 fp32 values of an optional vector (null: `otherwise`).
@@ -187,10 +192,10 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const T* __restrict__ X
 
 // part: [gridDim.x][2][C], the workgroup's sums of dgamma and dbeta (null: not wanted).
 template <typename T, int TPR, int VPT>
-__global__ __launch_bounds__(kBwdThreads) void norm_bwd_kernel(
+__global__ __launch_bounds__(bwd_threads(TPR)) void norm_bwd_kernel(
     const T* __restrict__ dY, const T* __restrict__ X, int64_t N, int64_t C, const float* __restrict__ gamma,
     const float* __restrict__ mean, const float* __restrict__ rstd, T* __restrict__ dX, float* __restrict__ part) {
-  constexpr int kTeams = kBwdThreads / TPR;
+  constexpr int kBwdThreads = bwd_threads(TPR), kTeams = kBwdThreads / TPR;
   __shared__ float red[2][2 * (kBwdThreads / 64)];
   extern __shared__ __attribute__((aligned(16))) float sums[];  // [kTeams / 2][2][TPR * VPT * 8]
   const int t = threadIdx.x % TPR, team = threadIdx.x / TPR;
@@ -372,8 +377,18 @@ __global__ __launch_bounds__(kSumCols * kSumGroups) void norm_sums_kernel(const 
   const int col = threadIdx.x % kSumCols, grp = threadIdx.x / kSumCols;
   const int64_t c = static_cast<int64_t>(blockIdx.x) * kSumCols + col;  // of the 2 C sums
   float v = 0.0f;
-  if (c < 2 * C)
-    for (int32_t p = grp; p < P; p += kSumGroups) v += part[static_cast<int64_t>(p) * 2 * C + c];
+  if (c < 2 * C) {
+    constexpr int kAhead = 8;  // loads in flight
+    int32_t p = grp;
+    for (; p + (kAhead - 1) * kSumGroups < P; p += kAhead * kSumGroups) {
+      float q[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) q[i] = part[static_cast<int64_t>(p + i * kSumGroups) * 2 * C + c];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) v += q[i];
+    }
+    for (; p < P; p += kSumGroups) v += part[static_cast<int64_t>(p) * 2 * C + c];
+  }
   red[grp][col] = v;
   __syncthreads();
   if (grp != 0 || c >= 2 * C) return;
@@ -387,7 +402,9 @@ __global__ __launch_bounds__(kSumCols * kSumGroups) void norm_sums_kernel(const 
 }
 
 constexpr int64_t kFwdMost = 16384, kBwdMost = 16384;  // longest rows kept in registers
-constexpr int kParts = kCUs;                           // partial weight gradients at most
+
+// Partial weight gradients at most: a workgroup of 16 waves a CU, two of 4 waves (short rows).
+int64_t most_parts(int64_t C) { return C <= 1024 ? 2 * kCUs : kCUs; }
 
 template <typename T, int TPR, int VPT>
 hipError_t fwd(const void* X, int64_t N, int64_t C, const float* gamma, const float* beta, float eps, void* Y,
@@ -417,18 +434,15 @@ hipError_t fwd_typed(const void* X, int64_t N, int64_t C, const float* gamma, co
 }
 
 // Workgroups of the backward kernel: the partial sums it leaves.
-int64_t bwd_parts(int64_t N, int64_t teams) {
-  const int64_t wgs = (N + teams - 1) / teams;
-  return wgs < kParts ? wgs : kParts;
-}
-int64_t bwd_teams(int64_t C) {
-  return C <= 1024 ? 16 : C <= 4096 ? 4 : C <= 8192 ? 2 : 1;
+int64_t bwd_parts(int64_t N, int64_t C) {
+  const int64_t teams = C <= 4096 ? 4 : C <= 8192 ? 2 : 1;
+  return std::min((N + teams - 1) / teams, most_parts(C));
 }
 
 template <typename T, int TPR, int VPT>
 hipError_t bwd(const void* dY, const void* X, int64_t N, int64_t C, const float* gamma, const float* mean,
                const float* rstd, void* dX, float* part, int64_t parts, hipStream_t s) {
-  constexpr int kTeams = kBwdThreads / TPR;
+  constexpr int kBwdThreads = bwd_threads(TPR), kTeams = kBwdThreads / TPR;
   constexpr int kLds = kTeams / 2 * 2 * TPR * VPT * 8 * 4;
   static std::atomic<int8_t> lds_set[kMaxDevices];
   const hipError_t e = set_lds_limit_once(lds_set, reinterpret_cast<const void*>(&norm_bwd_kernel<T, TPR, VPT>), kLds);
@@ -470,13 +484,13 @@ hipError_t launch_layernorm(const void* X, DType t, int64_t N, int64_t C, const 
 }
 
 int64_t layernorm_bwd_workspace(int64_t N, int64_t C) {
-  return (bwd_parts(N, bwd_teams(C)) * 2 * C + (C > kBwdMost ? 2 * N : 0)) * 4;
+  return (bwd_parts(N, C) * 2 * C + (C > kBwdMost ? 2 * N : 0)) * 4;
 }
 
 hipError_t launch_layernorm_bwd(const void* dY, const void* X, DType t, int64_t N, int64_t C, const float* gamma,
                                 const float* mean, const float* rstd, void* dX, float* dgamma, float* dbeta,
                                 void* workspace, hipStream_t s) {
-  const int64_t parts = bwd_parts(N, bwd_teams(C));
+  const int64_t parts = bwd_parts(N, C);
   float* part = static_cast<float*>(workspace);
   if (N > 0) {
     const hipError_t e = t == DType::F32 ? bwd_typed<float>(dY, X, N, C, gamma, mean, rstd, dX, part, parts, s)
