@@ -20,6 +20,13 @@ __device__ __forceinline__ T* global_ptr(V* p) {
   return (T*)(__attribute__((address_space(1))) T*)(p);
 }
 
+// The place of workgroup b of `grid` in an order in which those of one XCD
+// (b % 8, as the dispatcher deals them out) follow each other.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t b, uint32_t grid) {
+  const uint32_t x = b & 7u, rest = grid & 7u;
+  return x * (grid >> 3) + (x < rest ? x : rest) + (b >> 3);
+}
+
 // Eight consecutive elements: a unit of a row, and an operand fragment's share of a lane.
 template <typename T>
 struct Unit {

@@ -88,7 +88,7 @@ struct TParams {
   const float* bias;
   const void* residual;
   uint32_t nnb, nwb;  // tile counts along TN and TW
-  uint32_t grid8;     // grid / 8 when the grid is a multiple of 8, else 0
+  uint32_t grid;
 };
 
 // PL: packed units per lane that are loaded a chunk ahead; 0: more, loaded
@@ -115,13 +115,18 @@ __global__ __launch_bounds__(TEAMS * kThreads, TEAMS > 2 ? TEAMS : 2) void tile_
   // ---- tile of this workgroup: dispatch places workgroup b on XCD b % 8; L
   // numbers the workgroups of one XCD consecutively, in bands of four row
   // blocks x every weight block, so that an XCD's L2 holds few of either.
-  const uint32_t L = p.grid8 ? (blockIdx.x & 7u) * p.grid8 + (blockIdx.x >> 3) : blockIdx.x;
+  const uint32_t L = xcd_order(blockIdx.x, p.grid);
   const uint32_t per = 4u * p.nwb, band = L / per, within = L - band * per;
   const uint32_t rows = min(4u, p.nnb - 4u * band);
   const uint32_t wb = within / rows, nb = 4u * band + (within - wb * rows);
-  const int64_t n0 = static_cast<int64_t>(nb) * TN;
-  // first output of the tile along the weights: gated f, back c, plain and grad o
-  const int64_t w0 = static_cast<int64_t>(wb) * (MODE == kGated ? TW / 2 : TW);
+  // First row of X of the tile, and first output along the weights: gated f,
+  // back c, plain and grad o.  (Where columns of memory are the tile's, a last
+  // tile of fewer starts earlier and computes some again, in the same order: its
+  // loads are whole.)
+  const int64_t along = MODE == kGrad ? p.C : p.N, across = MODE == kBack ? p.C : p.O;
+  int64_t n0 = static_cast<int64_t>(nb) * TN, w0 = static_cast<int64_t>(wb) * (MODE == kGated ? TW / 2 : TW);
+  if constexpr (MODE == kGrad) n0 = max(min(n0, along - TN), static_cast<int64_t>(0));
+  if constexpr (MODE == kGrad || MODE == kBack) w0 = max(min(w0, across - TW), static_cast<int64_t>(0));
   const int64_t F = p.O / 2;
   constexpr bool kFwd = MODE == kGated || MODE == kPlain;
   const int64_t red = kFwd ? p.C : MODE == kBack ? p.O : p.N;  // reduction length
@@ -570,7 +575,7 @@ hipError_t launch(const TParams& q, hipStream_t s) {
   const uint32_t grid = static_cast<uint32_t>(nnb * nwb);
   p.nnb = static_cast<uint32_t>(nnb);
   p.nwb = static_cast<uint32_t>(nwb);
-  p.grid8 = grid % 8 == 0 ? grid / 8 : 0;
+  p.grid = grid;
   static std::atomic<int8_t> lds_set[kMaxDevices];
   const hipError_t e = set_lds_limit_once(lds_set, reinterpret_cast<const void*>(&tile_kernel<T, MODE, TN, TW, PL, TEAMS>), kLds);
   if (e != hipSuccess) return e;

@@ -41,7 +41,7 @@ struct SParams {
   void* pre;
   int64_t N, C, O;
   int32_t G, K, y_f32, act;
-  uint32_t nnb, nwb, grid8;
+  uint32_t nnb, nwb, grid;
 };
 
 constexpr int step_of(int wb) { return 128 / wb; }  // reduction elements of a step
@@ -81,7 +81,7 @@ __global__ __launch_bounds__(kThreads, 2) void wave_split_kernel(SParams p) {
 
   // ---- tile of this workgroup: dispatch places workgroup b on XCD b % 8; an
   // XCD's workgroups run through bands of four row blocks x every weight block
-  const uint32_t L = p.grid8 ? (blockIdx.x & 7u) * p.grid8 + (blockIdx.x >> 3) : blockIdx.x;
+  const uint32_t L = xcd_order(blockIdx.x, p.grid);
   const uint32_t per = 4u * p.nwb, band = L / per, within = L - band * per;
   const uint32_t rows = min(4u, p.nnb - 4u * band);
   const uint32_t wb = within / rows, nb = 4u * band + (within - wb * rows);
@@ -338,7 +338,7 @@ hipError_t launch(SParams p, hipStream_t s) {
   const uint32_t grid = static_cast<uint32_t>(nnb * nwb);
   p.nnb = static_cast<uint32_t>(nnb);
   p.nwb = static_cast<uint32_t>(nwb);
-  p.grid8 = grid % 8 == 0 ? grid / 8 : 0;
+  p.grid = grid;
   constexpr int kLds = kWaves * wave_lds(NT, WB) + 16;
   static std::atomic<int8_t> lds_set[kMaxDevices];
   const hipError_t e =

@@ -91,7 +91,6 @@ hipError_t launch_wide(const BlockProduct& a, int pt, hipStream_t s) {
   p.rows_w = 64 * a.K / a.G;
   const int64_t grid = static_cast<int64_t>(p.npb) * p.nob;
   if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
-  p.grid8 = grid % 8 == 0 ? static_cast<int32_t>(grid / 8) : 0;
   p.pgr = 6 * a.K < a.G ? 2 : 4;  // (as for the plain product)
   const bool ragged = q.red % kCK != 0 || q.out % q.tile != 0;
   const uint32_t g = static_cast<uint32_t>(grid);

@@ -252,7 +252,13 @@ __device__ __forceinline__ void wide_tile_body(const WParams& p, uint8_t* lds) {
   // one XCD consecutively, and runs of pgr * nob consecutive L cover pgr
   // pixel blocks x every output block, output-block-major.
   const uint32_t bid = blockIdx.x;
-  const uint32_t L = p.grid8 ? (bid & 7u) * static_cast<uint32_t>(p.grid8) + (bid >> 3) : bid;
+  uint32_t L;
+  if constexpr (MODE == kWPlain) {
+    L = p.grid8 ? (bid & 7u) * static_cast<uint32_t>(p.grid8) + (bid >> 3) : bid;
+  } else {  // (the same for grids that are no multiple of 8: the first ones of an XCD's run have one more)
+    const uint32_t x = bid & 7u, rest = gridDim.x & 7u;
+    L = x * (gridDim.x >> 3) + min(x, rest) + (bid >> 3);
+  }
   const uint32_t pgr = static_cast<uint32_t>(p.pgr);
   const uint32_t per = pgr * static_cast<uint32_t>(p.nob);
   const uint32_t pg = L / per;
