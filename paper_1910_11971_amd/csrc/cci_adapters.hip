@@ -18,8 +18,10 @@
 //           by 64 rows of B.  With bf16 operands T enters as the sum of two
 //           bf16 values (16 bits of mantissa): it is not rounded to one.
 // Fragments read from rows of memory cost the L1 one access per lane and 16
-// bytes; that and the latency of a chain of loads bind (3001 rows, C = O =
-// 4096, R = 32: FIGURES).
+// bytes; that and the latency of a chain of loads bind.  3001 rows, C = O =
+// 4096, R = 32, runs of 377 rows: shrink 13.9 us (18.8 with tiles of 16 rows),
+// expand 22.4, which writes 24.6 MB of D; 32 rows of 16 adapters, R = 16: 5.1
+// and 5.2, two launches' own time for the most part.
 #include <algorithm>
 #include <type_traits>
 

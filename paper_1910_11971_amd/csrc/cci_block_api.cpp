@@ -152,10 +152,8 @@ int wave_width(Kind kind) { return kind == kWave4 ? 4 : kind == kWave2 ? 2 : kin
 
 hipError_t gated_product(const BlockProduct& p, hipStream_t st) {
   if (p.t != DType::BF16) return launch_tile_gated(p, st);
-  // (Beyond a decoding batch the rows of X that a wave-split workgroup reads in fragments cost as much as they save:
-  // C = 4096, F = 8192: 32 rows 17 / 25 on 64 x 64 tiles, 64 rows 27 / 25; odd C more.)
   Choice c{kTiles, 1e30};
-  if (p.N <= 32) consider_wave_split(c, p, true);
+  consider_wave_split(c, p, true);  // (a decoding batch)
   if (c.kind == kTiles) c = tile_or_wide(p, p.C, p.O / 2, 32, 128, wide_gated_supports(p));
   if (const int wb = wave_width(c.kind)) return launch_wave_split(p, true, wb, st);
   return c.kind == kTiles ? launch_tile_gated(p, st) : launch_wide_gated(p, c.kind == kWide256 ? 8 : 4, st);

@@ -367,12 +367,13 @@ hipError_t launch_pl(const SParams& p, hipStream_t s) {
   return launch<MODE, NT, WB, 4, false>(p, s);
 }
 
-// Rows of a tile: as many as there are, 64 at most.
+// Rows of a tile: as many as there are, 64 at most (gated 32: see wave_split_supports).
 template <int MODE, int WB>
 hipError_t launch_wb(const SParams& p, hipStream_t s) {
   if (p.N <= 16) return launch_pl<MODE, 1, WB>(p, s);
   if (p.N <= 32) return launch_pl<MODE, 2, WB>(p, s);
-  return launch_pl<MODE, 4, WB>(p, s);
+  if constexpr (MODE == kBack) return launch_pl<MODE, 4, WB>(p, s);
+  return hipErrorInvalidConfiguration;
 }
 
 template <int MODE>
@@ -400,8 +401,11 @@ hipError_t launch_nt(const BlockProduct& a, int wb, hipStream_t s) {
 
 }  // namespace
 
+// (Gated, beyond a decoding batch: the rows of X that a workgroup reads in fragments cost as much as they save.
+// C = 4096, F = 8192, here / on 64 x 64 tiles: 32 rows 17 / 25 us, 64 rows 27 / 25; odd C more.)
 bool wave_split_supports(const BlockProduct& a, bool gated, int wb) {
-  return a.t == DType::BF16 && a.N >= 1 && units(gated, wb, a.G, a.K) <= 4 && (gated ? wb >= 2 : a.C >= 16 * wb);
+  return a.t == DType::BF16 && a.N >= 1 && units(gated, wb, a.G, a.K) <= 4 &&
+         (gated ? wb >= 2 && a.N <= 32 : a.C >= 16 * wb);
 }
 
 hipError_t launch_wave_split(const BlockProduct& a, bool gated, int wb, hipStream_t s) {

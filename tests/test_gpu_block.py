@@ -197,7 +197,8 @@ def test_layernorm_bwd_against_differences(cci):
 
 GATED_SIZES = [(1, 8, 8, 8, 2), (1, 64, 96, 16, 4), (3, 5, 6, 3, 2), (16, 128, 256, 16, 4), (17, 33, 40, 4, 1),
                (37, 520, 144, 16, 4), (64, 64, 64, 16, 4), (65, 72, 96, 32, 8), (130, 200, 256, 256, 3),
-               (33, 96, 512, 256, 256), (129, 64, 160, 16, 16), (200, 129, 130, 2, 1), (70, 1000, 48, 8, 8), (3333, 264, 1736, 8, 2), (1999, 448, 3104, 32, 20), (2500, 1000, 2544, 16, 16),
+               (33, 96, 512, 256, 256), (129, 64, 160, 16, 16), (200, 129, 130, 2, 1), (70, 1000, 48, 8, 8),
+               (3333, 264, 1736, 8, 2), (1999, 448, 3104, 32, 20), (2500, 1000, 2544, 16, 16),
                (2048, 512, 2560, 16, 4), (4100, 256, 1536, 64, 4),
                (90, 520, 512, 64, 40), (5, 1, 1, 1, 1), (2049, 136, 1032, 8, 2), (300, 256, 384, 16, 4),
                (2100, 64, 1100, 4, 2), (1024, 320, 2048, 32, 8)]
@@ -355,8 +356,9 @@ def test_non_finite_rows_stay_apart(cci):
 
 BACK_SIZES = [(1, 8, 8, 8, 2), (1, 4096, 64, 16, 4), (3, 6, 5, 3, 2), (64, 64, 64, 16, 4), (33, 96, 129, 32, 8),
               (100, 512, 200, 256, 7), (70, 256, 264, 256, 256), (2049, 72, 2050, 8, 2), (2048, 512, 2048, 16, 4),
-              (300, 1040, 512, 16, 16), (3333, 1736, 3400, 8, 2), (6001, 400, 2056, 16, 9),
-              (4096, 320, 3136, 2, 1), (4000, 640, 4000, 64, 64), (8192, 256, 1792, 16, 1), (257, 130, 131, 2, 1), (90, 960, 256, 64, 33), (40, 21, 1, 7, 3)]
+              (300, 1040, 512, 16, 16), (3333, 1736, 3400, 8, 2), (6001, 400, 2056, 16, 9), (4096, 320, 3136, 2, 1),
+              (4000, 640, 4000, 64, 64), (8192, 256, 1792, 16, 1), (257, 130, 131, 2, 1), (90, 960, 256, 64, 33),
+              (40, 21, 1, 7, 3)]
 
 
 @DTYPES
@@ -551,3 +553,87 @@ def test_other_stream(cci):
     side.synchronize()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def test_two_streams_at_once(cci):
+    """Calls in flight together have workspaces of their own."""
+    states = [block_state(cci, n, 6 + n) for n in (515, 700)]
+    want = [[o.clone() for o in block(cci, s, True) + block(cci, s, False)] for s in states]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in states]
+    for _ in range(3):
+        got = []
+        for s, q in zip(states, streams):
+            with torch.cuda.stream(q):
+                got.append(block(cci, s, True) + block(cci, s, False))
+        torch.cuda.synchronize()
+        for g, w in zip(got, want):
+            for a, b in zip(g, w):
+                assert torch.equal(a, b)
+
+
+# ------------------------------------------------- offsets past 32 bits --
+
+def test_long_layernorm(cci):
+    """4.3e9 elements: 1000 rows again and again, whose results are equal in every place."""
+    g, C, reps = gen(70), 8192, 530
+    X, dY, gamma = normal(g, 1000, C, dt=BF16), normal(g, 1000, C, dt=BF16), normal(g, C)
+    y0, m0, r0 = cci.layernorm(X, gamma)
+    d0, dg0, db0 = cci.layernorm_bwd(dY, X, m0, r0, gamma)
+    Xs, dYs = X.repeat(reps, 1), dY.repeat(reps, 1)
+    assert Xs.numel() > 2 ** 32
+    y, m, r = cci.layernorm(Xs, gamma)
+    d, dg, db = cci.layernorm_bwd(dYs, Xs, m, r, gamma)
+    for long, short in ((y, y0), (m, m0), (r, r0), (d, d0)):
+        assert (long.view(reps, *short.shape) == short).all()
+    # the sums: 1000 terms of reps equal ones, N u S with S the terms' magnitudes (and those of the short sums)
+    xh = ((X.double() - m0.double()[:, None]) * r0.double()[:, None])
+    for got, terms in ((dg, dY.double() * xh), (db, dY.double())):
+        within(got, reps * terms.sum(0), reps * terms.abs().sum(0) * (1000 * reps + 8) * U, "sums")
+
+
+@pytest.mark.parametrize("G,K,C", [(8, 1, 64), (4, 1, 61)])
+def test_long_products(cci, G, K, C):
+    """Rows of 8192 past element 2^32: the last thousand rows give what a thousand alone do."""
+    g, O, reps, B = gen(71), 8192, 530, 1000
+    F = O // 2
+    vals, idx, W = packed(cci, g, O, C, G, K, BF16)
+    X, dH = normal(g, B, C, dt=BF16), normal(g, B, F, dt=BF16)
+    Xs = X.repeat(reps, 1)
+    H, pre = cci.gated_spmm(Xs, vals, idx, G, act="silu", save_pre=True)
+    assert pre.numel() > 2 ** 32
+    P, S, ref, a = gated_ref(X, W, F, "silu")
+    e = (C + 2) * U * S
+    slack = 1.2 * e[:, :F] * (P[:, F:].abs() + e[:, F:]) + a.abs() * e[:, F:] + 16 * U * P[:, :F].abs() * P[:, F:].abs()
+    for k in (0, reps // 2, reps - 1):
+        rows = slice(B * k, B * (k + 1))
+        within(pre[rows], P, HALF[BF16] * P.abs() + e * (1 + HALF[BF16]), "pre")
+        within(H[rows], ref, HALF[BF16] * ref.abs() + slack * (1 + HALF[BF16]), "H")
+    dHs = dH.repeat(reps, 1)
+    dpre, dX, dv = cci.gated_spmm_bwd(dHs, pre, Xs, vals, idx, G, act="silu", dvals_dtype=F32)
+    assert (dpre.view(reps, B, O) == dpre[:B]).all()
+    d = dpre[:B].double()
+    for k in (0, reps - 1):
+        check_product(dX[B * k:B * (k + 1)], d, W, O, "dX")
+    x = X.double()
+    ref, mag = reps * (d.t() @ x), reps * (d.abs().t() @ x.abs())
+    at = idx.long()
+    take = lambda t: t.view(O // G, G, C).gather(1, at)
+    within(dv, take(ref), take(mag) * (B * reps + 8) * U, "dvals")
+    del dpre, dX, pre, H, dHs
+    L, R = 3, 5
+    A, Bw = normal(g, L, R, C, dt=BF16), normal(g, L, O, R, dt=BF16)
+    rows = torch.randint(-1, L, (B,), generator=g, device=DEV, dtype=torch.int32)
+    short = cci.spmm_adapters(X, vals, idx, G, A, Bw, rows)
+    Y = cci.spmm_adapters(Xs, vals, idx, G, A, Bw, rows.repeat(reps))
+    # (both within the bound of the short product; the kernels may differ with the number of rows)
+    w = W
+    T = torch.einsum("nrc,nc->nr", A.double()[rows.clamp_min(0).long()], x) * (rows >= 0).double()[:, None]
+    low = torch.einsum("nor,nr->no", Bw.double()[rows.clamp_min(0).long()], T)
+    Tm = torch.einsum("nrc,nc->nr", A.double()[rows.clamp_min(0).long()].abs(), x.abs())
+    lowm = torch.einsum("nor,nr->no", Bw.double()[rows.clamp_min(0).long()].abs(), Tm)
+    want, mags = x @ w.t() + low, x.abs() @ w.abs().t() + lowm
+    # D rounded once (2^-8), Y once; T enters with 16 bits (2^-16 of it), sums C + R terms
+    tol = HALF[BF16] * (want.abs() + 1.01 * low.abs()) * 1.01 + mags * ((C + R + 8) * U + 2.0 ** -16)
+    for got in (short, Y[:B], Y[-B:]):
+        within(got, want, tol, "adapters")
