@@ -47,7 +47,7 @@ inline int64_t groups_in(int64_t span, int64_t G) {
 // 16 wb weight rows (wb 4, 2; input gradients also 1): 8 wb outputs (gated) or
 // 16 wb columns.
 bool wave_split_supports(const BlockProduct& a, bool gated, int wb);
-hipError_t launch_wave_split(const BlockProduct& a, bool gated, int wb, hipStream_t s);
+hipError_t launch_wave_split(const BlockProduct& a, bool gated, int wb, int rows, hipStream_t s);
 // bf16 gated products and input gradients in tiles of 32 pt rows (pt 4 or 8)
 // x 128 outputs (gated) or 256 columns; 64 % G == 0, sizes in multiples of 8.
 bool wide_gated_supports(const BlockProduct& a);

@@ -96,15 +96,16 @@ bool tile_product(cci_dtype t, int64_t C, int64_t O, int32_t G) {
 // Which kernels run a bf16 gated product or input gradient.  Each family has a
 // time per piece of the reduction and round of workgroups over the 256 CUs,
 // measured on 90 shapes with G = 4 .. 32 and K / G = 1/4 and 1/2 (us):
-//   64 x 64 tiles, four teams of waves  1.3 a 4 chunks of 64, 3.5 a round
+//   64 x 64 tiles, four teams of waves  1.25 a 4 chunks of 64, 3.5 a round
 //   64 x 64 tiles, one team             0.95 a chunk for up to 1024 tiles
 //   128 x 128 tiles                     1.1 a chunk, 1.4 for 257 .. 512 tiles, and so on by 512
 //   wide tiles, 128 rows                1.07 a chunk, 256 rows 1.42
-//   wave-split                          0.3 per row block and 32 elements of a step of its eight waves, 0.55 at
-//                                       least, 4 a round
+//   wave-split                          kSteps: a step of its eight waves, a round
 // Both sides of the borders (tile / wide 128 / wide 256 / wave-split):
-//   gated, C = 4096, F = 8192: 128 rows 48 / 68 / 94 / 51, 256 rows 70 / 69 / 95 / 96, 1024 rows 171 / 134 / 103 / 360;
+//   gated, C = 4096, F = 8192: 32 rows 25 / - / - / 17, 64 rows 24 / - / - / 28, 128 rows 48 / 68 / 94 / 51, 256 rows
+//   70 / 69 / 95 / 96, 1024 rows 171 / 134 / 103 / 360; C = 2928, F = 4704, 70 rows 36 / - / - / 20;
 //   dX, O = 8192, C = 4096: 256 rows 50 / 136 / 182 / 45, 1024 rows 144 / 137 / 181 / 164, 2048 rows 190 / 142 / 181 / 309.
+// On 41 drawn shapes of up to 3400 rows the choice takes 1.01 times the best form's time (dX).
 
 double rounds(int64_t tiles, int64_t at_once) { return static_cast<double>((tiles + at_once - 1) / at_once); }
 
@@ -112,9 +113,10 @@ enum Kind { kTiles, kWide128, kWide256, kWave4, kWave2, kWave1 };
 struct Choice {
   Kind kind;
   double us;
+  int rows;  // wave-split: of a tile
 };
-void consider(Choice& best, Kind kind, double us) {
-  if (us < best.us) best = Choice{kind, us};
+void consider(Choice& best, Kind kind, double us, int rows = 0) {
+  if (us < best.us) best = Choice{kind, us, rows};
 }
 
 // out: the outputs of a row, per64 / per256: those of a 64- and a 256-row weight tile.
@@ -123,9 +125,11 @@ Choice tile_or_wide(const BlockProduct& p, int64_t red, int64_t out, int64_t per
   const int64_t t64 = (p.N + 63) / 64 * ((out + per64 - 1) / per64);
   const int64_t t128 = (p.N + 127) / 128 * ((out + 2 * per64 - 1) / (2 * per64));
   const double teams = static_cast<double>((red + 255) / 256);
-  Choice best{kTiles, 4.0 + (t128 >= 256   ? chunks * (t128 <= 256 ? 1.1 : 1.4 * rounds(t128, 512))
-                        : t64 <= 512 ? rounds(t64, 256) * (teams * 1.3 + 3.5)
-                                     : chunks * 0.95)};
+  Choice best{kTiles,
+              t128 >= 256  ? 4.0 + chunks * (t128 <= 256 ? 1.1 : 1.4 * rounds(t128, 512))
+              : t64 <= 512 ? 1.0 + rounds(t64, 256) * (teams * 1.25 + 3.5)
+                           : 4.0 + chunks * 0.95,
+              0};
   if (wide) {
     const int64_t w = (out + per256 - 1) / per256;
     consider(best, kWide128, 4.0 + chunks * 1.07 * rounds((p.N + 127) / 128 * w, 256));
@@ -134,17 +138,29 @@ Choice tile_or_wide(const BlockProduct& p, int64_t red, int64_t out, int64_t per
   return best;
 }
 
-// The best of the wave-split kernels' tile widths.
+// The best of the wave-split kernels' tiles (blocks of 16 rows, nt, and of weights, wb): us a step, a round and a
+// call.  Half the rows take more than half the time, but fill the CUs where tiles are few, and two workgroups of the
+// narrowest tile share a CU (short rounds).  64 / 32 rows, dX: 333 x 1000 -> 2728 19.2 / 11.4, 777 x 5456 -> 1000
+// 29.5 / 35.1, 1424 x 3584 -> 160 22.9 / 15.5.
+struct StepTime {
+  double step, round, call;
+};
+constexpr StepTime kSteps[3][3] = {{{0.55, 4.0, 5.0}, {0.6, 4.0, 5.0}, {1.2, 4.0, 5.0}},    // nt = 1: wb = 4, 2, 1
+                                   {{0.62, 1.5, 3.7}, {0.85, 6.0, 1.0}, {1.6, 6.0, 1.5}},    // nt = 2
+                                   {{0.98, 5.0, 1.0}, {1.75, 4.8, 1.0}, {3.4, 6.0, 1.0}}};   // nt = 4
 void consider_wave_split(Choice& best, const BlockProduct& p, bool gated) {
   const int64_t red = gated ? p.C : p.O, out = gated ? p.O / 2 : p.C;
-  const int64_t nt = p.N <= 16 ? 1 : p.N <= 32 ? 2 : 4;  // blocks of 16 rows
-  for (const int wb : {4, 2, 1}) {
-    if (!wave_split_supports(p, gated, wb)) continue;
-    const int64_t ks = 128 / wb;  // elements of a step
-    const double step = std::max(0.55, 0.3 * static_cast<double>(nt * ks / 32));
-    const double steps = static_cast<double>((red + 8 * ks - 1) / (8 * ks));
-    const int64_t width = (gated ? 8 : 16) * wb, tiles = (p.N + 16 * nt - 1) / (16 * nt) * ((out + width - 1) / width);
-    consider(best, wb == 4 ? kWave4 : wb == 2 ? kWave2 : kWave1, 5.0 + rounds(tiles, 256) * (steps * step + 4.0));
+  const int most = p.N <= 16 ? 1 : p.N <= 32 || gated ? 2 : 4;  // blocks of 16 rows
+  for (int nt = most; nt >= (most == 4 ? 2 : most); nt -= 2) {
+    for (const int wb : {4, 2, 1}) {
+      if (!wave_split_supports(p, gated, wb)) continue;
+      const int64_t ks = 128 / wb;  // elements of a step
+      const StepTime& t = kSteps[nt / 2][wb == 4 ? 0 : wb == 2 ? 1 : 2];
+      const double steps = static_cast<double>((red + 8 * ks - 1) / (8 * ks));
+      const int64_t width = (gated ? 8 : 16) * wb, tiles = (p.N + 16 * nt - 1) / (16 * nt) * ((out + width - 1) / width);
+      consider(best, wb == 4 ? kWave4 : wb == 2 ? kWave2 : kWave1,
+               t.call + rounds(tiles, 256) * (steps * t.step + t.round), 16 * nt);
+    }
   }
 }
 
@@ -152,10 +168,9 @@ int wave_width(Kind kind) { return kind == kWave4 ? 4 : kind == kWave2 ? 2 : kin
 
 hipError_t gated_product(const BlockProduct& p, hipStream_t st) {
   if (p.t != DType::BF16) return launch_tile_gated(p, st);
-  Choice c{kTiles, 1e30};
-  consider_wave_split(c, p, true);  // (a decoding batch)
-  if (c.kind == kTiles) c = tile_or_wide(p, p.C, p.O / 2, 32, 128, wide_gated_supports(p));
-  if (const int wb = wave_width(c.kind)) return launch_wave_split(p, true, wb, st);
+  Choice c = tile_or_wide(p, p.C, p.O / 2, 32, 128, wide_gated_supports(p));
+  consider_wave_split(c, p, true);
+  if (const int wb = wave_width(c.kind)) return launch_wave_split(p, true, wb, c.rows, st);
   return c.kind == kTiles ? launch_tile_gated(p, st) : launch_wide_gated(p, c.kind == kWide256 ? 8 : 4, st);
 }
 
@@ -163,7 +178,7 @@ hipError_t input_gradient(const BlockProduct& p, hipStream_t st) {
   if (p.t != DType::BF16) return launch_tile_back(p, st);
   Choice c = tile_or_wide(p, p.O, p.C, 64, 256, wide_back_supports(p));
   consider_wave_split(c, p, false);
-  if (const int wb = wave_width(c.kind)) return launch_wave_split(p, false, wb, st);
+  if (const int wb = wave_width(c.kind)) return launch_wave_split(p, false, wb, c.rows, st);
   return c.kind == kTiles ? launch_tile_back(p, st) : launch_wide_back(p, c.kind == kWide256 ? 8 : 4, st);
 }
 

@@ -15,7 +15,9 @@
 // at the end, added in the order of the waves.
 // The LDS binds: a step is 4 zeroing stores, 8 per unit of kept entries and 4
 // fragment reads, about 180 cycles whatever NT is.  Fewer rows than a tile
-// holds cost nothing more, narrow tiles (WB) fill the CUs when there are few.
+// holds cost nothing more; narrow tiles (WB) or fewer rows (NT) fill the CUs
+// when there are few tiles (dX, 333 x 1000 -> 2728: 19.2 us on 258 tiles of 64
+// rows, 11.4 on 473 of 32).
 //
 // Weight tile rows: gated 8 WB gate rows, then the up rows of the same
 // outputs; back: columns c, the reduction element along the row.  LDS:
@@ -367,17 +369,17 @@ hipError_t launch_pl(const SParams& p, hipStream_t s) {
   return launch<MODE, NT, WB, 4, false>(p, s);
 }
 
-// Rows of a tile: as many as there are, 64 at most (gated 32: see wave_split_supports).
+// rows: of a tile, 16, 32 or (back) 64.
 template <int MODE, int WB>
-hipError_t launch_wb(const SParams& p, hipStream_t s) {
-  if (p.N <= 16) return launch_pl<MODE, 1, WB>(p, s);
-  if (p.N <= 32) return launch_pl<MODE, 2, WB>(p, s);
+hipError_t launch_wb(const SParams& p, int rows, hipStream_t s) {
+  if (rows == 16) return launch_pl<MODE, 1, WB>(p, s);
+  if (rows == 32) return launch_pl<MODE, 2, WB>(p, s);
   if constexpr (MODE == kBack) return launch_pl<MODE, 4, WB>(p, s);
   return hipErrorInvalidConfiguration;
 }
 
 template <int MODE>
-hipError_t launch_nt(const BlockProduct& a, int wb, hipStream_t s) {
+hipError_t launch_nt(const BlockProduct& a, int wb, int rows, hipStream_t s) {
   SParams p{};
   p.X = MODE == kGated ? a.X : a.dY;
   p.vals = a.vals;
@@ -391,25 +393,23 @@ hipError_t launch_nt(const BlockProduct& a, int wb, hipStream_t s) {
   p.K = a.K;
   p.y_f32 = a.y_t == DType::F32;
   p.act = static_cast<int32_t>(a.act);
-  if (wb == 4) return launch_wb<MODE, 4>(p, s);
-  if (wb == 2) return launch_wb<MODE, 2>(p, s);
+  if (wb == 4) return launch_wb<MODE, 4>(p, rows, s);
+  if (wb == 2) return launch_wb<MODE, 2>(p, rows, s);
   if constexpr (MODE == kBack) {
-    if (wb == 1) return launch_wb<MODE, 1>(p, s);
+    if (wb == 1) return launch_wb<MODE, 1>(p, rows, s);
   }
   return hipErrorInvalidConfiguration;
 }
 
 }  // namespace
 
-// (Gated, beyond a decoding batch: the rows of X that a workgroup reads in fragments cost as much as they save.
-// C = 4096, F = 8192, here / on 64 x 64 tiles: 32 rows 17 / 25 us, 64 rows 27 / 25; odd C more.)
 bool wave_split_supports(const BlockProduct& a, bool gated, int wb) {
   return a.t == DType::BF16 && a.N >= 1 && units(gated, wb, a.G, a.K) <= 4 &&
-         (gated ? wb >= 2 && a.N <= 32 : a.C >= 16 * wb);
+         (gated ? wb >= 2 : a.C >= 16 * wb);
 }
 
-hipError_t launch_wave_split(const BlockProduct& a, bool gated, int wb, hipStream_t s) {
-  return gated ? launch_nt<kGated>(a, wb, s) : launch_nt<kBack>(a, wb, s);
+hipError_t launch_wave_split(const BlockProduct& a, bool gated, int wb, int rows, hipStream_t s) {
+  return gated ? launch_nt<kGated>(a, wb, rows, s) : launch_nt<kBack>(a, wb, rows, s);
 }
 
 }  // namespace cci

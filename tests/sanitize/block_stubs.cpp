@@ -32,9 +32,9 @@ hipError_t launch_tile_plain(const BlockProduct&, hipStream_t) { return reached(
 hipError_t launch_tile_back(const BlockProduct&, hipStream_t) { return reached(); }
 hipError_t launch_tile_grad(const BlockProduct&, hipStream_t) { return reached(); }
 bool wave_split_supports(const BlockProduct& a, bool gated, int wb) {
-  return a.t == DType::BF16 && (gated ? wb >= 2 && a.N <= 32 : a.C >= 16 * wb);
+  return a.t == DType::BF16 && (gated ? wb >= 2 : a.C >= 16 * wb);
 }
-hipError_t launch_wave_split(const BlockProduct&, bool, int, hipStream_t) { return reached(); }
+hipError_t launch_wave_split(const BlockProduct&, bool, int, int, hipStream_t) { return reached(); }
 bool wide_gated_supports(const BlockProduct& a) { return a.t == DType::BF16 && a.C % 8 == 0 && a.O % 16 == 0; }
 hipError_t launch_wide_gated(const BlockProduct&, int, hipStream_t) { return reached(); }
 bool wide_back_supports(const BlockProduct& a) { return a.t == DType::BF16 && a.C % 8 == 0 && a.O % 8 == 0; }
