@@ -121,6 +121,33 @@ cci_algo ragged_route(cci::ProductArgs& a, cci_algo chosen, bool mac_next) {
   return chosen;
 }
 
+// AUTO's choice for a product.  mac_next: one that the dense-tile kernels
+// refuse goes to the sparse-MAC ones.
+cci_algo auto_route(cci::ProductArgs& a, bool& mac_next) {
+  const int64_t cin = a.conv ? a.geom.Cin : a.C;
+  cci_algo chosen = cci_auto_algo(a.x_t == cci::DType::F32 ? CCI_F32 : CCI_BF16,
+                                  a.val_t == cci::DType::F32 ? CCI_F32 : CCI_BF16, a.N, a.C, cin, a.O, a.G, a.K);
+  // (the shape-only choice cannot see stride, padding and alignment)
+  bool ok = true;
+  switch (chosen) {
+    case CCI_ALGO_FEW_ROWS_MFMA: ok = few_rows_ok(a); break;
+    case CCI_ALGO_RESIDENT_MFMA: ok = cci::resident_supports(a); break;
+    case CCI_ALGO_WIDE_TILE_MFMA: ok = cci::wide_tile_supports(a); break;
+    case CCI_ALGO_NARROW_MFMA: ok = cci::narrow_supports(a); break;
+    case CCI_ALGO_TAP_TILE_MFMA: ok = cci::tap_tile_supports(a); break;
+    case CCI_ALGO_STREAM_TILE_MFMA: ok = cci::stream_tile_supports(a); break;
+    case CCI_ALGO_SPLIT_K_MFMA: ok = cci::split_k_supports(a); break;
+    default: break;
+  }
+  if (!ok) {
+    const bool tap = (chosen == CCI_ALGO_WIDE_TILE_MFMA || chosen == CCI_ALGO_STREAM_TILE_MFMA) &&
+                     cci::tap_tile_supports(a);
+    mac_next = !tap && chosen != CCI_ALGO_WIDE_TILE_MFMA;
+    chosen = tap ? CCI_ALGO_TAP_TILE_MFMA : CCI_ALGO_DENSE_TILE_MFMA;
+  }
+  return ragged_route(a, chosen, mac_next);
+}
+
 cci_status run_product(cci::ProductArgs& a, cci_algo algo, const cci_epilogue* ep,
                        void* stream) {
   a.scale = ep ? ep->scale : nullptr;
@@ -138,32 +165,8 @@ cci_status run_product(cci::ProductArgs& a, cci_algo algo, const cci_epilogue* e
   if (a.N == 0) return ok();
 
   cci_algo chosen = algo;
-  bool mac_next = false;  // AUTO: a product the dense-tile kernels refuse goes to the sparse-MAC ones
-  if (algo == CCI_ALGO_AUTO) {
-    const int64_t cin = a.conv ? a.geom.Cin : a.C;
-    chosen = cci_auto_algo(a.x_t == cci::DType::F32 ? CCI_F32 : CCI_BF16,
-                           a.val_t == cci::DType::F32 ? CCI_F32 : CCI_BF16, a.N, a.C, cin, a.O,
-                           a.G, a.K);
-    // (the shape-only choice cannot see stride, padding and alignment)
-    bool ok = true;
-    switch (chosen) {
-      case CCI_ALGO_FEW_ROWS_MFMA: ok = few_rows_ok(a); break;
-      case CCI_ALGO_RESIDENT_MFMA: ok = cci::resident_supports(a); break;
-      case CCI_ALGO_WIDE_TILE_MFMA: ok = cci::wide_tile_supports(a); break;
-      case CCI_ALGO_NARROW_MFMA: ok = cci::narrow_supports(a); break;
-      case CCI_ALGO_TAP_TILE_MFMA: ok = cci::tap_tile_supports(a); break;
-      case CCI_ALGO_STREAM_TILE_MFMA: ok = cci::stream_tile_supports(a); break;
-      case CCI_ALGO_SPLIT_K_MFMA: ok = cci::split_k_supports(a); break;
-      default: break;
-    }
-    if (!ok) {
-      const bool tap = (chosen == CCI_ALGO_WIDE_TILE_MFMA || chosen == CCI_ALGO_STREAM_TILE_MFMA) &&
-                       cci::tap_tile_supports(a);
-      mac_next = !tap && chosen != CCI_ALGO_WIDE_TILE_MFMA;
-      chosen = tap ? CCI_ALGO_TAP_TILE_MFMA : CCI_ALGO_DENSE_TILE_MFMA;
-    }
-  }
-  if (algo == CCI_ALGO_AUTO) chosen = ragged_route(a, chosen, mac_next);
+  bool mac_next = false;
+  if (algo == CCI_ALGO_AUTO) chosen = auto_route(a, mac_next);
   if (chosen == CCI_ALGO_DENSE_TILE_MFMA && !cci::dense_tile_supports(a)) {
     if (!mac_next)
       return fail(CCI_EUNSUPPORTED,
@@ -259,6 +262,14 @@ cci_status to_2of4(bool from_cci, const void* vals, cci_dtype val_t, const uint8
 }
 
 }  // namespace
+
+namespace cci {
+bool spmm_without_matrix_cores(ProductArgs a) {
+  bool mac_next = false;
+  const cci_algo chosen = auto_route(a, mac_next);
+  return chosen == CCI_ALGO_SPARSE_MAC || (chosen == CCI_ALGO_DENSE_TILE_MFMA && !dense_tile_supports(a));
+}
+}  // namespace cci
 
 extern "C" {
 

@@ -84,12 +84,32 @@ size_t adapter_d_bytes(int64_t N, int64_t O, cci_dtype y_t) {
   return (static_cast<size_t>(N) * static_cast<size_t>(O) * dsize(y_t) + 15) / 16 * 16;
 }
 
-// cci_spmm runs a product on kernels made for its shape, except where rows
-// are not a multiple of 8 elements long (bf16: the vector ALUs, which do 1/32
-// of the matrix cores' rate) and for groups that it refuses.
-bool tile_product(cci_dtype t, int64_t C, int64_t O, int32_t G) {
-  const bool mac = G == 2 || G == 4 || G == 8 || G == 16 || G == 32;
-  return !mac || (t == CCI_BF16 && (C % 8 != 0 || O % 8 != 0));
+// cci_spmm runs a product on kernels made for its shape, except in bf16 what
+// it leaves to the vector ALUs, at 1/32 of the matrix cores' rate (239 x 3896
+// -> 416, G = 32, K = 8: 271 us there, 28 here), and groups that it refuses.
+// Rows that are not a multiple of 8 elements long have a form there that reads
+// element by element.
+bool tile_product(const BlockProduct& p) {
+  if (p.t == DType::F32) return p.G != 2 && p.G != 4 && p.G != 8 && p.G != 16 && p.G != 32;
+  if (p.C % 8 != 0 || p.O % 8 != 0) return true;
+  ProductArgs a{};
+  a.X = p.X;
+  a.x_t = a.val_t = p.t;
+  a.N = p.N;
+  a.C = p.C;
+  a.conv = false;
+  a.vals = p.vals;
+  a.idx = p.idx;
+  a.O = p.O;
+  a.G = p.G;
+  a.K = p.K;
+  a.Y = p.Y;
+  a.y_t = p.y_t;
+  a.scale = p.scale;
+  a.bias = p.bias;
+  a.residual = p.residual;
+  a.relu = p.relu;
+  return spmm_without_matrix_cores(a);
 }
 
 // ---------------------------------------------------------------------------
@@ -360,8 +380,6 @@ cci_status cci_spmm_adapters(const void* X, cci_dtype x_t, int64_t N, int64_t C,
   const hipStream_t st = static_cast<hipStream_t>(stream);
   if (cci_status s = launched(launch_adapters(a, st), "adapter")) return s;
   cci_epilogue with{ep ? ep->scale : nullptr, ep ? ep->bias : nullptr, workspace, ep ? ep->relu : 0};
-  if (!tile_product(x_t, C, O, G))
-    return cci_spmm(X, x_t, N, C, vals, val_t, idx, O, G, K, &with, Y, y_t, stream);
   BlockProduct p{};
   p.X = X;
   p.t = to_dt(x_t);
@@ -378,6 +396,7 @@ cci_status cci_spmm_adapters(const void* X, cci_dtype x_t, int64_t N, int64_t C,
   p.bias = with.bias;
   p.residual = with.residual;
   p.relu = with.relu;
+  if (!tile_product(p)) return cci_spmm(X, x_t, N, C, vals, val_t, idx, O, G, K, &with, Y, y_t, stream);
   return launched(launch_tile_plain(p, st), "product");
 }
 

@@ -31,6 +31,7 @@ hipError_t launch_tile_gated(const BlockProduct&, hipStream_t) { return reached(
 hipError_t launch_tile_plain(const BlockProduct&, hipStream_t) { return reached(); }
 hipError_t launch_tile_back(const BlockProduct&, hipStream_t) { return reached(); }
 hipError_t launch_tile_grad(const BlockProduct&, hipStream_t) { return reached(); }
+bool spmm_without_matrix_cores(ProductArgs a) { return a.C % 32 != 0; }
 bool wave_split_supports(const BlockProduct& a, bool gated, int wb) {
   return a.t == DType::BF16 && (gated ? wb >= 2 : a.C >= 16 * wb);
 }

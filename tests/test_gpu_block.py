@@ -381,8 +381,9 @@ def test_spmm_t(cci, i, size, dt):
 ADAPTER_SIZES = [(1, 8, 8, 8, 2, 1, 1), (1, 4096, 256, 16, 4, 4, 16), (32, 512, 256, 16, 4, 16, 16),
                  (64, 256, 128, 8, 2, 100, 8), (37, 96, 130, 2, 1, 3, 5), (200, 72, 200, 8, 2, 5, 64),
                  (333, 129, 48, 4, 1, 7, 33), (100, 64, 66, 3, 2, 2, 16), (1000, 320, 264, 8, 4, 9, 100),
-                 (50, 1000, 256, 64, 8, 3, 4), (2, 33, 21, 7, 7, 2, 257), (150, 64, 200, 8, 2, 3, 600), (70, 160, 90, 2, 1, 2, 48),
-                 (500, 544, 96, 16, 4, 70, 16), (65, 31, 65, 5, 2, 1, 1024)]
+                 (50, 1000, 256, 64, 8, 3, 4), (2, 33, 21, 7, 7, 2, 257), (150, 64, 200, 8, 2, 3, 600),
+                 (70, 160, 90, 2, 1, 2, 48), (500, 544, 96, 16, 4, 70, 16), (65, 31, 65, 5, 2, 1, 1024),
+                 (239, 3896, 416, 32, 8, 5, 32)]
 
 
 @DTYPES
