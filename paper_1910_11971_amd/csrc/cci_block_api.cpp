@@ -89,8 +89,12 @@ size_t adapter_d_bytes(int64_t N, int64_t O, cci_dtype y_t) {
 // -> 416, G = 32, K = 8: 271 us there, 28 here), and groups that it refuses.
 // Rows that are not a multiple of 8 elements long have a form there that reads
 // element by element.
+// In fp32 it has the vector ALUs alone, which are ahead for few rows; with the
+// adapters' own kernels, tiles / that product alone: 8 rows 640 -> 352 24 / 10,
+// 4096 -> 4096 (G = 16, K = 4) 106 / 44; 64 rows 26 / 11 and 109 / 293; 429
+// rows 30 / 393 and 209 / 2714; 2000 rows 2048 -> 2048, G = 32, K = 1, 201 / 799.
 bool tile_product(const BlockProduct& p) {
-  if (p.t == DType::F32) return p.G != 2 && p.G != 4 && p.G != 8 && p.G != 16 && p.G != 32;
+  if (p.t == DType::F32) return p.N > 32 || (p.G != 2 && p.G != 4 && p.G != 8 && p.G != 16 && p.G != 32);
   if (p.C % 8 != 0 || p.O % 8 != 0) return true;
   ProductArgs a{};
   a.X = p.X;
