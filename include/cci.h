@@ -513,17 +513,18 @@ typedef struct {
   int32_t R;
 } cci_adapters;
 
-/* Bytes of the workspace of cci_spmm_adapters (the adapters' term in Y's
- * type and the partial sums of A . x). */
+/* Bytes of the workspace of cci_spmm_adapters (the product in fp32, of up to
+ * 1 GiB of rows at a time, and the partial sums of A . x); the same for
+ * either y_t. */
 cci_status cci_spmm_adapters_workspace(int64_t N, int64_t C, int64_t O,
                                        int64_t L, int32_t R, cci_dtype y_t,
                                        size_t *bytes);
 
 /* The product of cci_spmm with a low-rank term per row:
- *   D[n][o] = residual[n][o] + alpha[a] * sum_r B[a][o][r] (A[a][r] . X[n]),
- *   Y[n][o] = relu?( acc * scale[o] + bias[o] + D[n][o] ),
- * acc the CCI product; D is rounded to Y's type before it is added.  Types
- * as for cci_spmm; G may be any from 1 to 256.  Rows may come in any order;
+ *   D[n][o] = alpha[a] * sum_r B[a][o][r] (A[a][r] . X[n]),
+ *   Y[n][o] = relu?( acc * scale[o] + bias[o] + residual[n][o] + D[n][o] ),
+ * acc the CCI product.  The terms are added in fp32 and Y is rounded once.
+ * residual may be Y itself.  Types as for cci_spmm; G may be any from 1 to 256.  Rows may come in any order;
  * rows of one request next to each other share its weights' reads.  The sums
  * run in a fixed order.  Non-finite values as for cci_spmm's bf16 families;
  * those of one adapter reach its rows alone. */

@@ -1,8 +1,12 @@
 // Low-rank adapters of many requests: for row n with adapter a = rows[n],
-//   D[n][o] = residual[n][o] + alpha[a] sum_r T[n][r] B[a][o][r],  T[n][r] = sum_c A[a][r][c] X[n][c];
-// a row whose adapter is outside [0, L) gets the residual alone.  The shared
-// projection then takes D as its residual, so the sum is rounded once more
-// than the projection alone (D, in the output's type, is a small part of it).
+//   D[n][o] = P[n][o] + residual[n][o] + alpha[a] sum_r T[n][r] B[a][o][r],  T[n][r] = sum_c A[a][r][c] X[n][c],
+// P the shared projection; a row whose adapter is outside [0, L) has no third
+// term.  P comes in fp32 and the sum is rounded once, to D's type: the
+// adapters' term and the residual are as large as the projection, and where
+// they cancel a sum of rounded terms would be off by far more than a rounding
+// of its own.  (The other order, the projection adding a term that this file
+// had left in the output's type, moves 50 MB less over 3001 x 4096 outputs in
+// bf16, 131 us for the call and 140 now, and doubled the outputs' rounding.)
 //
 // Both kernels work on tiles of 16 RT rows and walk over the distinct adapters
 // among them: the matrix cores multiply all rows by one adapter, and the rows
@@ -20,8 +24,8 @@
 // Fragments read from rows of memory cost the L1 one access per lane and 16
 // bytes; that and the latency of a chain of loads bind.  3001 rows, C = O =
 // 4096, R = 32, runs of 377 rows: shrink 13.9 us (18.8 with tiles of 16 rows),
-// expand 22.4, which writes 24.6 MB of D; 32 rows of 16 adapters, R = 16: 5.1
-// and 5.2, two launches' own time for the most part.
+// expand 27.7, which reads 49 MB of P and writes 24.6 of D; 32 rows of 16 adapters, R = 16: 4.6
+// and 5.4, two launches' own time for the most part.
 #include <algorithm>
 #include <type_traits>
 
@@ -47,11 +51,12 @@ struct AParams {
   const void* B;
   const float* alpha;
   const int32_t* rows;
-  const void* residual;
+  const float* base;     // P
+  const void* residual;  // of D's type
   void* D;
   float* part;  // [S][N][R]
   int64_t N, C, O, L, cols;
-  int32_t R, S, P, d_f32;
+  int32_t R, S, P, d_f32, relu;
 };
 
 // The adapter of row n (-1: none).
@@ -221,6 +226,15 @@ __device__ __forceinline__ Split split(const float (&t)[8]) {
   return s;
 }
 
+// An output from its terms: the projection, the residual at `at` (if it is there) and the adapter's.
+__device__ __forceinline__ float total(const AParams& p, float base, int64_t at, bool there, float term) {
+  float v = base;
+  if (p.residual && there)
+    v += p.d_f32 ? global_ptr<const float>(p.residual)[at] : bf16_to_f32(global_ptr<const uint16_t>(p.residual)[at]);
+  v += term;
+  return p.relu && v <= 0.0f ? 0.0f : v;  // (a NaN stays)
+}
+
 // A workgroup has 16 RT rows and every `groups`-th block of 256 outputs.
 template <typename T, int RT>
 __global__ __launch_bounds__(kThreads) void expand_kernel(AParams p, uint32_t nob, uint32_t groups) {
@@ -316,14 +330,11 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AParams p, uint32_t no
 #pragma unroll
       for (int b = 0; b < kOutBlocks; ++b) {
         const int64_t o = o0 + 16 * b + 4 * lq, at = n * p.O + o;
+        f32x4_t base;
+        load_elems<4>(base, global_ptr<const float>(p.base) + at, p.O - o);
         float v[4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          v[r] = out[b][t][r];
-          if (p.residual && o + r < p.O)
-            v[r] += p.d_f32 ? global_ptr<const float>(p.residual)[at + r]
-                            : bf16_to_f32(global_ptr<const uint16_t>(p.residual)[at + r]);
-        }
+        for (int r = 0; r < 4; ++r) v[r] = total(p, base[r], at + r, o + r < p.O, out[b][t][r]);
         if (p.d_f32)
           store4<float>(global_ptr<float>(p.D) + at, v, p.O - o, vec);
         else
@@ -360,8 +371,7 @@ __global__ __launch_bounds__(kThreads) void expand_rows_kernel(AParams p, uint32
   }
   if (o >= p.O) return;
   const int64_t at = n * p.O + o;
-  if (p.residual)
-    v += p.d_f32 ? global_ptr<const float>(p.residual)[at] : bf16_to_f32(global_ptr<const uint16_t>(p.residual)[at]);
+  v = total(p, global_ptr<const float>(p.base)[at], at, true, v);
   if (p.d_f32)
     global_ptr<float>(p.D)[at] = v;
   else
@@ -433,7 +443,9 @@ hipError_t launch_adapters(const AdapterArgs& a, hipStream_t s) {
   p.B = a.B;
   p.alpha = a.alpha;
   p.rows = a.rows;
+  p.base = a.base;
   p.residual = a.residual;
+  p.relu = a.relu;
   p.D = a.D;
   p.part = a.part;
   p.N = a.N;

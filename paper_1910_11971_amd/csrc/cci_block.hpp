@@ -33,10 +33,8 @@ struct BlockProduct {
   void* Y;             // gated: H [N][O/2]; plain: [N][O]; back: dX [N][C]; grad: dvals [O/G][K][C]
   void* pre;           // gated: preactivations [N][O], or null
   DType y_t;           // plain, back, grad: type of Y
-  const float* scale;  // plain: the epilogue of cci_spmm
+  const float* scale;  // plain: Y = (X . W_hat^T) * scale + bias (each may be null)
   const float* bias;
-  const void* residual;
-  int32_t relu;
 };
 // Groups that meet any `span` rows starting at a multiple of it.
 inline int64_t groups_in(int64_t span, int64_t G) {
@@ -71,8 +69,8 @@ hipError_t launch_grad_mfma_to(const void* dY, const void* X, int64_t N, int64_t
 hipError_t launch_gate_grad(const void* dH, const void* pre, DType t, int64_t N, int64_t F, Act act, void* dpre,
                             hipStream_t s);
 
-// Low-rank adapters: D[n][o] = residual[n][o] + alpha[a] sum_r (sum_c A[a][r][c] X[n][c]) B[a][o][r], a = rows[n]
-// (outside [0, L): the residual alone).
+// Low-rank adapters: D[n][o] = relu?(base[n][o] + residual[n][o] + alpha[a] sum_r (sum_c A[a][r][c] X[n][c]) B[a][o][r]),
+// a = rows[n] (outside [0, L): without the third term).
 struct AdapterArgs {
   const void* X;
   DType t;
@@ -82,7 +80,9 @@ struct AdapterArgs {
   const void* B;
   const float* alpha;
   const int32_t* rows;
-  const void* residual;
+  const float* base;     // the shared projection
+  const void* residual;  // of D's type, or null; D may be the same memory
+  int32_t relu;
   void* D;
   DType d_t;
   float* part;  // workspace of adapter_part_bytes()

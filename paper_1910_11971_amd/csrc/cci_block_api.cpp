@@ -80,8 +80,21 @@ cci_status check_adapters(int64_t N, int64_t C, int64_t O, int64_t L, int32_t R)
   return check_rows(N, C > O ? C : O);
 }
 
-size_t adapter_d_bytes(int64_t N, int64_t O, cci_dtype y_t) {
-  return (static_cast<size_t>(N) * static_cast<size_t>(O) * dsize(y_t) + 15) / 16 * 16;
+// Rows that a call takes at a time.  The projection waits in the workspace in
+// fp32 for its adapters' term; slices keep that at 1 GiB, and inside the
+// 32-bit offsets of the kernels that cci_spmm runs large products on.
+int64_t adapter_slice(int64_t N, int64_t O) { return std::min(N, std::max<int64_t>(256, (int64_t(1) << 28) / O / 256 * 256)); }
+
+size_t adapter_base_bytes(int64_t N, int64_t O) {
+  return (static_cast<size_t>(adapter_slice(N, O)) * static_cast<size_t>(O) * sizeof(float) + 15) / 16 * 16;
+}
+
+// Projection and partial sums of a slice, whole or the last one.
+size_t adapter_workspace(int64_t N, int64_t C, int64_t O, int64_t L, int32_t R) {
+  if (N == 0) return 0;
+  const int64_t rows = adapter_slice(N, O), last = N % rows;
+  const int64_t part = std::max(adapter_part_bytes(rows, C, L, R), last ? adapter_part_bytes(last, C, L, R) : 0);
+  return adapter_base_bytes(N, O) + static_cast<size_t>(part);
 }
 
 // cci_spmm runs a product on kernels made for its shape, except in bf16 what
@@ -111,8 +124,6 @@ bool tile_product(const BlockProduct& p) {
   a.y_t = p.y_t;
   a.scale = p.scale;
   a.bias = p.bias;
-  a.residual = p.residual;
-  a.relu = p.relu;
   return spmm_without_matrix_cores(a);
 }
 
@@ -340,7 +351,7 @@ cci_status cci_spmm_adapters_workspace(int64_t N, int64_t C, int64_t O, int64_t 
   if (!dtype_ok(y_t)) return fail(CCI_EINVAL, "unknown dtype code");
   if (cci_status s = check_adapters(N, C, O, L, R)) return s;
   if (!bytes) return fail(CCI_EINVAL, "null output pointer");
-  *bytes = N == 0 ? 0 : adapter_d_bytes(N, O, y_t) + static_cast<size_t>(adapter_part_bytes(N, C, L, R));
+  *bytes = adapter_workspace(N, C, O, L, R);
   return ok();
 }
 
@@ -361,14 +372,26 @@ cci_status cci_spmm_adapters(const void* X, cci_dtype x_t, int64_t N, int64_t C,
       !aligned16(adapters->B) || !aligned16(adapters->rows) || misaligned(adapters->alpha) || misaligned(workspace) ||
       (ep && (misaligned(ep->scale) || misaligned(ep->bias) || misaligned(ep->residual))))
     return fail(CCI_EALIGN, "pointer not 16-byte aligned");
-  const size_t d_bytes = adapter_d_bytes(N, O, y_t);
-  const size_t need = d_bytes + static_cast<size_t>(adapter_part_bytes(N, C, adapters->L, adapters->R));
+  const size_t need = adapter_workspace(N, C, O, adapters->L, adapters->R);
   if (!workspace || workspace_bytes < need)
     return fail(CCI_EINVAL, "workspace of %zu bytes, %zu needed", workspace ? workspace_bytes : 0, need);
+  // the projection in fp32, then the adapters' term and the one rounding to Y's type
+  float* base = static_cast<float*>(workspace);
+  const cci_epilogue affine{ep ? ep->scale : nullptr, ep ? ep->bias : nullptr, nullptr, 0};
+  BlockProduct p{};
+  p.t = to_dt(x_t);
+  p.C = C;
+  p.vals = vals;
+  p.idx = idx;
+  p.O = O;
+  p.G = G;
+  p.K = K;
+  p.Y = base;
+  p.y_t = DType::F32;
+  p.scale = affine.scale;
+  p.bias = affine.bias;
   AdapterArgs a{};
-  a.X = X;
-  a.t = to_dt(x_t);
-  a.N = N;
+  a.t = p.t;
   a.C = C;
   a.O = O;
   a.L = adapters->L;
@@ -376,32 +399,25 @@ cci_status cci_spmm_adapters(const void* X, cci_dtype x_t, int64_t N, int64_t C,
   a.A = adapters->A;
   a.B = adapters->B;
   a.alpha = adapters->alpha;
-  a.rows = adapters->rows;
-  a.residual = ep ? ep->residual : nullptr;
-  a.D = workspace;
+  a.base = base;
+  a.relu = ep ? ep->relu : 0;
   a.d_t = to_dt(y_t);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + d_bytes);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + adapter_base_bytes(N, O));
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  if (cci_status s = launched(launch_adapters(a, st), "adapter")) return s;
-  cci_epilogue with{ep ? ep->scale : nullptr, ep ? ep->bias : nullptr, workspace, ep ? ep->relu : 0};
-  BlockProduct p{};
-  p.X = X;
-  p.t = to_dt(x_t);
-  p.N = N;
-  p.C = C;
-  p.vals = vals;
-  p.idx = idx;
-  p.O = O;
-  p.G = G;
-  p.K = K;
-  p.Y = Y;
-  p.y_t = to_dt(y_t);
-  p.scale = with.scale;
-  p.bias = with.bias;
-  p.residual = with.residual;
-  p.relu = with.relu;
-  if (!tile_product(p)) return cci_spmm(X, x_t, N, C, vals, val_t, idx, O, G, K, &with, Y, y_t, stream);
-  return launched(launch_tile_plain(p, st), "product");
+  const int64_t slice = adapter_slice(N, O);
+  for (int64_t n = 0; n < N; n += slice) {
+    p.X = a.X = static_cast<const char*>(X) + static_cast<size_t>(n * C) * dsize(x_t);
+    p.N = a.N = std::min(slice, N - n);
+    a.rows = adapters->rows + n;
+    a.residual = ep && ep->residual ? static_cast<const char*>(ep->residual) + static_cast<size_t>(n * O) * dsize(y_t) : nullptr;
+    a.D = static_cast<char*>(Y) + static_cast<size_t>(n * O) * dsize(y_t);
+    const cci_status s =
+        tile_product(p) ? launched(launch_tile_plain(p, st), "product")
+                        : cci_spmm(p.X, x_t, p.N, C, vals, val_t, idx, O, G, K, &affine, base, CCI_F32, stream);
+    if (s != CCI_OK) return s;
+    if (const cci_status t = launched(launch_adapters(a, st), "adapter")) return t;
+  }
+  return ok();
 }
 
 }  // extern "C"

@@ -2,7 +2,7 @@
 // any sizes, groups and alignment of rows, in bf16 and fp32:
 //   gated  H[n][f] = act(P[n][f]) P[n][F + f],  P = X . W_hat^T, the gate and
 //          up weights one packing of the stacked [2F][C] matrix;
-//   plain  Y = epilogue(X . W_hat^T);
+//   plain  Y = X . W_hat^T * scale + bias, in fp32;
 //   back   dX[n][c] = sum_o dY[n][o] W_hat[o][c];
 //   grad   dvals[g][k][c] = sum_n dY[n][gG + idx[g][k][c]] X[n][c].
 // All but the last expand each chunk of packed groups to a dense tile in LDS
@@ -88,11 +88,10 @@ struct TParams {
   void* pre;
   int64_t N, C, O;
   int32_t G, K;
-  int32_t y_f32;     // plain, back, grad: Y (and residual) is fp32
-  int32_t act, relu;
+  int32_t y_f32;     // back, grad: Y is fp32
+  int32_t act;
   const float* scale;
   const float* bias;
-  const void* residual;
   uint32_t nnb, nwb;  // tile counts along TN and TW
   uint32_t grid;
 };
@@ -506,15 +505,8 @@ __global__ __launch_bounds__(TEAMS * kThreads, TEAMS > 2 ? TEAMS : 2) void tile_
           if (c + r >= p.O) continue;
           if (p.scale) v[r] *= global_ptr<const float>(p.scale)[c + r];
           if (p.bias) v[r] += global_ptr<const float>(p.bias)[c + r];
-          if (p.residual)
-            v[r] += p.y_f32 ? global_ptr<const float>(p.residual)[at + r]
-                            : bf16_to_f32(global_ptr<const uint16_t>(p.residual)[at + r]);
-          if (p.relu) v[r] = v[r] > 0.0f ? v[r] : (v[r] != v[r] ? v[r] : 0.0f);
         }
-        if (p.y_f32)
-          store4<float>(global_ptr<float>(p.Y) + at, v, p.O - c, vec);
-        else
-          store4<bf16_t>(global_ptr<bf16_t>(p.Y) + at, v, p.O - c, vec);
+        store4<float>(global_ptr<float>(p.Y) + at, v, p.O - c, vec);
       }
     }
   } else if constexpr (MODE == kBack) {
@@ -635,8 +627,6 @@ TParams params(const BlockProduct& a) {
   p.act = static_cast<int32_t>(a.act);
   p.scale = a.scale;
   p.bias = a.bias;
-  p.residual = a.residual;
-  p.relu = a.relu;
   return p;
 }
 

@@ -1,0 +1,83 @@
+"""Outputs of the feed-forward block's operators held to the rounding that
+their definitions leave, where a looser bound would pass a wrong step.
+
+Tolerances are those of test_gpu_block.py: u = 2^-24 per term of an fp32 sum,
+half a step of the output's type for its one rounding.
+"""
+import pytest
+import torch
+
+from gpu_common import DEV, Guarded
+from test_gpu_block import BF16, F32, F64, HALF, U, cci, gen, normal, packed, within  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- adapters --
+
+def adapter_terms(X, W, A, B, rows, alpha):
+    """Product, adapters' term, and the magnitudes of the terms of either, in 64 bits."""
+    x = X.double()
+    acc, S = x @ W.t(), x.abs() @ W.abs().t()
+    D, SD = torch.zeros_like(acc), torch.zeros_like(acc)
+    for a in range(A.shape[0]):
+        n = (rows == a).nonzero()[:, 0]
+        f = alpha[a].double()
+        D[n] = f * (x[n] @ A[a].double().t()) @ B[a].double().t()
+        SD[n] = f.abs() * (x[n].abs() @ A[a].double().abs().t()) @ B[a].double().abs().t()
+    return acc, S, D, SD
+
+
+def check_adapters(got, X, W, A, B, rows, alpha, res, relu, what):
+    """One rounding to the output's type: T enters a bf16 product in two parts (2^-16 of each term), the three terms
+    are added in fp32 (u of each partial sum)."""
+    C, R = X.shape[1], A.shape[1]
+    acc, S, D, SD = adapter_terms(X, W, A, B, rows, alpha)
+    r = res.double()
+    ref = acc + r + D
+    e = ((C + 8) * U * S + ((C + R + 24) * U + (2.0 ** -16 if X.dtype == BF16 else 0.0)) * SD
+         + 4 * U * (S + SD + r.abs()))
+    if relu:
+        ref = ref.clamp_min(0)
+    within(got, ref, HALF[got.dtype] * ref.abs() + e * (1 + HALF[got.dtype]), what)
+
+
+@pytest.mark.parametrize("dt,y_t", [(BF16, BF16), (BF16, F32), (F32, F32)], ids=["bf16", "bf16-f32", "f32"])
+@pytest.mark.parametrize("size", [(1, 256, 256, 16, 4, 3, 16), (40, 512, 256, 16, 4, 5, 16), (200, 256, 264, 8, 2, 4, 32),
+                                  (333, 129, 48, 4, 1, 7, 33), (70, 320, 66, 3, 2, 3, 8)])
+def test_adapters_round_once(cci, size, dt, y_t):  # noqa: F811
+    N, C, O, G, K, L, R = size
+    g = gen(N)
+    X, A, B = normal(g, N, C, dt=dt), normal(g, L, R, C, dt=dt, std=C ** -0.5), normal(g, L, O, R, dt=dt, std=R ** -0.5)
+    vals, idx, W = packed(cci, g, O, C, G, K, dt)
+    rows = torch.randint(-1, L, (N,), generator=g, device=DEV, dtype=torch.int32)
+    alpha = 1 + normal(g, L, std=0.1)
+    # a residual that all but cancels the other terms: what was rounded before the sum would stand out
+    acc, _, D, _ = adapter_terms(X, W, A, B, rows, alpha)
+    for res, relu in ((normal(g, N, O, dt=y_t, std=4.0), False), ((-(acc + D)).to(y_t), False), (normal(g, N, O, dt=y_t), True)):
+        out = Guarded((N, O), y_t)
+        got = cci.spmm_adapters(X, vals, idx, G, A, B, rows, alpha=alpha, residual=res, relu=relu, out_dtype=y_t, out=out.t)
+        torch.cuda.synchronize()
+        check_adapters(got, X, W, A, B, rows, alpha, res, relu, f"relu {relu}")
+        out.check("adapters")
+        # the residual may be the output
+        same = res.clone()
+        cci.spmm_adapters(X, vals, idx, G, A, B, rows, alpha=alpha, residual=same, relu=relu, out_dtype=y_t, out=same)
+        assert torch.equal(same, got)
+
+
+def test_adapters_in_slices_of_rows(cci):  # noqa: F811
+    """Outputs so wide that a call's rows go through the workspace in two slices."""
+    N, C, O, G, K, L, R = 300, 8, 1 << 20, 8, 2, 3, 4
+    g = gen(1)
+    X, A, B = normal(g, N, C, dt=BF16), normal(g, L, R, C, dt=BF16), normal(g, L, O, R, dt=BF16, std=0.5)
+    vals, idx, W = packed(cci, g, O, C, G, K, BF16)
+    rows = torch.randint(-1, L, (N,), generator=g, device=DEV, dtype=torch.int32)
+    alpha, res = 1 + normal(g, L, std=0.1), normal(g, N, O, dt=BF16)
+    out = Guarded((N, O), BF16)
+    cci.spmm_adapters(X, vals, idx, G, A, B, rows, alpha=alpha, residual=res, out=out.t)
+    torch.cuda.synchronize()
+    for n in range(0, N, 50):
+        s = slice(n, n + 50)
+        check_adapters(out.t[s], X[s], W, A, B, rows[s], alpha, res[s], False, f"rows {n}")
+    out.check("adapters")
