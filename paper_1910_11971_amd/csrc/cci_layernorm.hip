@@ -68,6 +68,12 @@ __device__ __forceinline__ void team_sum(float (&v)[NV], float* red) {
   }
 }
 
+// 1 / sqrt(var + eps); a variance below 0 is rounding, and a NaN stays one.
+__device__ __forceinline__ float deviation(float var, float eps) { return 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps); }
+
+// The mean from its first value and what that left out (of an infinite one: a NaN).
+__device__ __forceinline__ float whole_mean(float m, float lost) { return __builtin_isfinite(m) ? m + lost : m; }
+
 template <typename T, int TPR, int VPT>
 __global__ __launch_bounds__(kFwdThreads > TPR ? kFwdThreads : TPR) void norm_kernel(
     const T* __restrict__ X, int64_t N, int64_t C, const float* __restrict__ gamma, const float* __restrict__ beta,
@@ -115,7 +121,7 @@ __global__ __launch_bounds__(kFwdThreads > TPR ? kFwdThreads : TPR) void norm_ke
     }
     team_sum<TPR, kThreads>(sq, red2);
     const float lost = sq[0] / len;
-    const float r = 1.0f / sqrtf(fmaxf(sq[1] / len - lost * lost, 0.0f) + eps);
+    const float r = deviation(sq[1] / len - lost * lost, eps);
     if (!on) continue;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
@@ -130,7 +136,7 @@ __global__ __launch_bounds__(kFwdThreads > TPR ? kFwdThreads : TPR) void norm_ke
       }
     }
     if (t == 0) {
-      if (mean) mean[n] = m + lost;
+      if (mean) mean[n] = whole_mean(m, lost);
       if (rstd) rstd[n] = r;
     }
   }
@@ -168,7 +174,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const T* __restrict__ X
     }
     team_sum<1024, 1024>(sq, red2);
     const float lost = sq[0] / len;
-    const float r = 1.0f / sqrtf(fmaxf(sq[1] / len - lost * lost, 0.0f) + eps);
+    const float r = deviation(sq[1] / len - lost * lost, eps);
     for (int64_t c = 8 * threadIdx.x; c < C; c += 8 * 1024) {
       Unit<T> u;
       float ga[8], be[8];
@@ -184,7 +190,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(const T* __restrict__ X
       }
     }
     if (threadIdx.x == 0) {
-      if (mean) mean[n] = m + lost;
+      if (mean) mean[n] = whole_mean(m, lost);
       if (rstd) rstd[n] = r;
     }
   }

@@ -81,3 +81,27 @@ def test_adapters_in_slices_of_rows(cci):  # noqa: F811
         s = slice(n, n + 50)
         check_adapters(out.t[s], X[s], W, A, B, rows[s], alpha, res[s], False, f"rows {n}")
     out.check("adapters")
+
+
+# -------------------------------------------------------------- layer norm --
+
+@pytest.mark.parametrize("dt", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("C", [1, 40, 1500, 16392])
+@pytest.mark.parametrize("eps", [1e-5, 0.0])
+def test_layernorm_statistics_of_non_finite_rows(cci, C, dt, eps):  # noqa: F811
+    """mean and rstd are the formulas' for rows that hold infinities or NaN, and the other rows' stay."""
+    inf, nan = float("inf"), float("nan")
+    X = (normal(gen(C), 6, C) + 1).to(dt)
+    clean = X.clone()
+    for n, v in ((1, inf), (2, -inf), (4, nan)):
+        X[n, C // 2] = v
+    if C > 1:
+        X[5, 0], X[5, C - 1] = inf, -inf
+    Y, mean, rstd = cci.layernorm(X, eps=eps)
+    want = X.double().mean(1)
+    assert mean[1] == inf and mean[2] == -inf and mean[4].isnan()
+    for n in (1, 2, 4) + ((5,) if C > 1 else ()):
+        assert torch.equal(mean[n].isnan(), want[n].isnan()) and rstd[n].isnan() and Y[n].isnan().all(), n
+    for got, alone in zip((Y, mean, rstd), cci.layernorm(clean, eps=eps)):
+        for n in (0, 3):
+            assert torch.equal(got[n].isnan(), alone[n].isnan()) and torch.equal(got[n].nan_to_num(7), alone[n].nan_to_num(7))
