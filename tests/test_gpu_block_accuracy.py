@@ -105,3 +105,17 @@ def test_layernorm_statistics_of_non_finite_rows(cci, C, dt, eps):  # noqa: F811
     for got, alone in zip((Y, mean, rstd), cci.layernorm(clean, eps=eps)):
         for n in (0, 3):
             assert torch.equal(got[n].isnan(), alone[n].isnan()) and torch.equal(got[n].nan_to_num(7), alone[n].nan_to_num(7))
+
+
+@pytest.mark.parametrize("dt", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("C", [776, 4096, 16392])
+def test_layernorm_mean_is_as_good_as_a_sum(cci, C, dt):  # noqa: F811
+    """Means of rows of deviation 1, on average over 2000 rows.  A sum in fp32 whose partial sums grow as sqrt(k) (k up
+    to 64 in a thread, then 10 levels that each hold C terms in all) is off by u / sqrt(3) of every partial sum, at
+    random: by less than u sqrt((32 + 10) C / 3) in all, 3.8 u / sqrt(C) of the mean.  The mean's own rounding adds half
+    a step of it, u |m| at most; deviations that lose the same part for every x would add up to u."""
+    X = (normal(gen(C), 2000, C) + normal(gen(C + 1), 2000, 1, std=0.1)).to(dt)
+    mean = cci.layernorm(X)[1].double()
+    want = X.double().mean(1)
+    off = (mean - want).abs().mean().item()
+    assert off <= U * (3.8 / C ** 0.5 + want.abs().mean().item()), off / U
