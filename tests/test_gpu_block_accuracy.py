@@ -4,11 +4,13 @@ their definitions leave, where a looser bound would pass a wrong step.
 Tolerances are those of test_gpu_block.py: u = 2^-24 per term of an fp32 sum,
 half a step of the output's type for its one rounding.
 """
+import math
+
 import pytest
 import torch
 
 from gpu_common import DEV, Guarded
-from test_gpu_block import BF16, F32, F64, HALF, U, cci, gen, normal, packed, within  # noqa: F401
+from test_gpu_block import ACTS, BF16, F32, F64, HALF, U, cci, gen, normal, packed, within  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -119,3 +121,59 @@ def test_layernorm_mean_is_as_good_as_a_sum(cci, C, dt):  # noqa: F811
     want = X.double().mean(1)
     off = (mean - want).abs().mean().item()
     assert off <= U * (3.8 / C ** 0.5 + want.abs().mean().item()), off / U
+
+
+# -------------------------------------------------------------- activations --
+
+def act_parts(x, name):
+    """act(x) and act'(x) in 64 bits without cancellation in the tails, the magnitudes of the slope's terms, and the
+    size of the argument of the exponential in them."""
+    if name == "gelu":
+        # (torch.special.ndtr is 0 from -8.3 on, where Phi is 5e-17)
+        c, q = torch.special.erfc(x * -0.5 ** 0.5) / 2, torch.exp(-x * x / 2) / math.sqrt(2 * math.pi)
+        return x * c, c + x * q, c + (x * q).abs(), x * x
+    if name in ("silu", "gelu_tanh"):
+        k = math.sqrt(8 / math.pi)
+        z, dz = (x, 1.0) if name == "silu" else (k * (x + 0.044715 * x ** 3), k * (1 + 0.134145 * x * x))
+        s, e = torch.sigmoid(z), torch.sigmoid(z) * torch.sigmoid(-z)
+        return x * s, s + x * e * dz, s + (x * e * dz).abs(), z.abs()
+    return (x.clamp_min(0), (x > 0).double(), (x > 0).double(), 0 * x) if name == "relu" else (x, torch.ones_like(x), torch.ones_like(x), 0 * x)
+
+
+@pytest.mark.parametrize("dt", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("act", ACTS)
+def test_activation_tails(cci, act, dt):  # noqa: F811
+    """Values and slopes from -12 to 12 beside a large up value, relative to themselves.  An exponential's argument z
+    comes with up to 6 u of its size, 16 u are the library functions' and 8 the products'; below 1e-35 they underflow."""
+    F, up = 2048, 1000.0
+    x = torch.linspace(-12, 12, F, device=DEV).to(dt)
+    W = torch.cat((x.float(), torch.full((F,), up, device=DEV))).view(-1, 1)
+    vals, idx = cci.pack(W, 1, 1, dt)
+    X = torch.tensor([[1.0], [-1.0], [0.5]], device=DEV, dtype=dt)
+    H, pre = cci.gated_spmm(X, vals, idx, 1, act=act, save_pre=True)
+    p = X.double() * W.double().t()
+    assert torch.equal(pre.double(), p)  # powers of two times values of the type
+    g, u = p[:, :F], p[:, F:]
+    a, d, terms, z = act_parts(g, act)
+    rel = (6 * z + 24) * U
+    within(H, a * u, (a * u).abs() * (HALF[dt] + rel) * (1 + HALF[dt]) + 1e-35 * up, "H")
+    dH = torch.full_like(H, 3.0)
+    dpre, _, _ = cci.gated_spmm_bwd(dH, pre, X, vals, idx, 1, act=act)
+    within(dpre[:, F:], 3 * a, (3 * a).abs() * (HALF[dt] + rel) * (1 + HALF[dt]) + 1e-35, "du")
+    within(dpre[:, :F], 3 * u * d, (3 * u * d).abs() * HALF[dt] + 3 * u.abs() * terms * rel * (1 + HALF[dt]) + 1e-35 * up, "dg")
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_far_out(cci, act):  # noqa: F811
+    """Arguments whose square or cube overflows: the activations are 0 or the argument there, their slopes 0 or 1."""
+    g = torch.tensor([3e4, 1e20, 3e38, -3e4, -1e20, -3e38, 0.0], device=DEV)
+    F = g.numel()
+    vals, idx = cci.pack(torch.cat((g, torch.full((F,), 0.5, device=DEV))).view(-1, 1), 1, 1, F32)
+    X = torch.ones((1, 1), device=DEV)
+    H, pre = cci.gated_spmm(X, vals, idx, 1, act=act, save_pre=True)
+    dpre, _, _ = cci.gated_spmm_bwd(torch.ones_like(H), pre, X, vals, idx, 1, act=act)
+    none = act == "none"
+    a = g if none else g.clamp_min(0)
+    at0 = {"none": 1.0, "relu": 0.0}.get(act, 0.5)
+    d = torch.where(g == 0, at0, ((g > 0) | none).float())
+    assert torch.equal(H[0], 0.5 * a) and torch.equal(dpre[0, F:], a) and torch.equal(dpre[0, :F], 0.5 * d)
