@@ -444,7 +444,8 @@ cci_status cci_layernorm_bwd_workspace(int64_t N, int64_t C, size_t *bytes);
  * dX [N][C] of t, dgamma and dbeta fp32 [C]; each may be NULL.  N == 0
  * writes zeros to dgamma and dbeta.  The sums run in a fixed order: equal
  * calls give equal bits.  workspace: device memory that nothing else uses
- * until the call's work is done. */
+ * until the call's work is done; not used, and may be NULL, where dgamma and
+ * dbeta are NULL and C <= 16384. */
 cci_status cci_layernorm_bwd(const void *dY, const void *X, cci_dtype t,
                              int64_t N, int64_t C, const float *gamma,
                              const float *mean, const float *rstd, void *dX,

@@ -538,9 +538,10 @@ def layernorm_bwd(dY: torch.Tensor, X: torch.Tensor, mean: torch.Tensor, rstd: t
     if gamma is not None:
         _tensor(gamma, "gamma", (C,), torch.float32, dev)
     code = _code(X.dtype)
-    nb = _sz()
-    _check(_lib.cci_layernorm_bwd_workspace(N, C, ctypes.byref(nb)))
-    ws = torch.empty(nb.value, dtype=torch.uint8, device=dev)
+    nb, ws = _sz(), None
+    if need_dw or C > 16384:  # (shorter rows alone need none)
+        _check(_lib.cci_layernorm_bwd_workspace(N, C, ctypes.byref(nb)))
+        ws = torch.empty(nb.value, dtype=torch.uint8, device=dev)
     dX = torch.empty_like(X) if need_dx else None
     dg, db = (torch.empty(C, dtype=torch.float32, device=dev) if need_dw else None for _ in range(2))
     back = _enter(dev)

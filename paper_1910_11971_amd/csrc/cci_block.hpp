@@ -14,6 +14,9 @@ enum class Act { NONE = 0, RELU = 1, SILU = 2, GELU = 3, GELU_TANH = 4 };
 // Layer norm over the last dimension.
 hipError_t launch_layernorm(const void* X, DType t, int64_t N, int64_t C, const float* gamma, const float* beta,
                             float eps, void* Y, float* mean, float* rstd, hipStream_t s);
+// The backward pass keeps rows of up to so many elements in registers; it needs no workspace for them where the weight
+// gradients (dgamma and dbeta) are not wanted.
+constexpr int64_t kNormBwdMost = 16384;
 int64_t layernorm_bwd_workspace(int64_t N, int64_t C);
 hipError_t launch_layernorm_bwd(const void* dY, const void* X, DType t, int64_t N, int64_t C, const float* gamma,
                                 const float* mean, const float* rstd, void* dX, float* dgamma, float* dbeta,

@@ -245,7 +245,7 @@ cci_status cci_layernorm_bwd(const void* dY, const void* X, cci_dtype t, int64_t
                              void* workspace, size_t workspace_bytes, void* stream) {
   if (cci_status s = check_norm(t, N, C)) return s;
   if (N > 0 && (!dY || !X || !mean || !rstd)) return fail(CCI_EINVAL, "null pointer");
-  const size_t need = static_cast<size_t>(layernorm_bwd_workspace(N, C));
+  const size_t need = dgamma || dbeta || C > kNormBwdMost ? static_cast<size_t>(layernorm_bwd_workspace(N, C)) : 0;
   if (need > 0 && (!workspace || workspace_bytes < need))
     return fail(CCI_EINVAL, "workspace of %zu bytes, %zu needed", workspace ? workspace_bytes : 0, need);
   if (misaligned(dY) || misaligned(X) || misaligned(gamma) || misaligned(mean) || misaligned(rstd) || misaligned(dX) ||

@@ -359,7 +359,7 @@ __global__ __launch_bounds__(256) void norm_bwd_cols_kernel(
   load_vec(ga, gamma, c, C - c, 1.0f);
   const int64_t end = min(N, (rb + 1) * rows);
   for (int64_t n = rb * rows; n < end; ++n) {
-    const float m = mean[n], r = rstd[n], c1 = stats[2 * n], c2 = stats[2 * n + 1];
+    const float m = mean[n], r = rstd[n], c1 = dX ? stats[2 * n] : 0.0f, c2 = dX ? stats[2 * n + 1] : 0.0f;
     Unit<T> x, y;
     load_elems<8>(x, X + n * C + c, C - c);
     load_elems<8>(y, dY + n * C + c, C - c);
@@ -419,7 +419,7 @@ __global__ __launch_bounds__(kSumCols * kSumGroups) void norm_sums_kernel(const 
   }
 }
 
-constexpr int64_t kFwdMost = 16384, kBwdMost = 16384;  // longest rows kept in registers
+constexpr int64_t kFwdMost = 16384;  // longest rows kept in registers (backward: kNormBwdMost)
 
 // Partial weight gradients at most: a workgroup of 16 waves a CU, two of 4 waves (short rows).
 int64_t most_parts(int64_t C) { return C <= 1024 ? 2 * kCUs : kCUs; }
@@ -473,8 +473,8 @@ hipError_t bwd(const void* dY, const void* X, int64_t N, int64_t C, const float*
 
 template <typename T>
 hipError_t bwd_typed(const void* dY, const void* X, int64_t N, int64_t C, const float* gamma, const float* mean,
-                     const float* rstd, void* dX, float* part, int64_t parts, hipStream_t s) {
-  if (C <= kBwdMost) {
+                     const float* rstd, void* dX, float* part, float* stats, int64_t parts, hipStream_t s) {
+  if (C <= kNormBwdMost) {
     if (C <= 512) return bwd<T, 64, 1>(dY, X, N, C, gamma, mean, rstd, dX, part, parts, s);
     if (C <= 1024) return bwd<T, 64, 2>(dY, X, N, C, gamma, mean, rstd, dX, part, parts, s);
     if (C <= 2048) return bwd<T, 256, 1>(dY, X, N, C, gamma, mean, rstd, dX, part, parts, s);
@@ -482,10 +482,11 @@ hipError_t bwd_typed(const void* dY, const void* X, int64_t N, int64_t C, const 
     if (C <= 8192) return bwd<T, 512, 2>(dY, X, N, C, gamma, mean, rstd, dX, part, parts, s);
     return bwd<T, 1024, 2>(dY, X, N, C, gamma, mean, rstd, dX, part, parts, s);
   }
-  float* stats = part + parts * 2 * C;
-  hipLaunchKernelGGL((norm_bwd_rows_kernel<T>), dim3(static_cast<uint32_t>(N < 65536 ? N : 65536)), dim3(1024), 0, s,
-                     static_cast<const T*>(dY), static_cast<const T*>(X), N, C, gamma, mean, rstd, stats);
-  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  if (dX) {  // the weight gradients do not need the rows' means
+    hipLaunchKernelGGL((norm_bwd_rows_kernel<T>), dim3(static_cast<uint32_t>(N < 65536 ? N : 65536)), dim3(1024), 0, s,
+                       static_cast<const T*>(dY), static_cast<const T*>(X), N, C, gamma, mean, rstd, stats);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
   const int64_t rows = (N + parts - 1) / parts, cb = (C + 2047) / 2048;
   hipLaunchKernelGGL((norm_bwd_cols_kernel<T>), dim3(static_cast<uint32_t>(parts * cb)), dim3(256), 0, s,
                      static_cast<const T*>(dY), static_cast<const T*>(X), N, C, gamma, mean, rstd, stats,
@@ -502,20 +503,23 @@ hipError_t launch_layernorm(const void* X, DType t, int64_t N, int64_t C, const 
 }
 
 int64_t layernorm_bwd_workspace(int64_t N, int64_t C) {
-  return (bwd_parts(N, C) * 2 * C + (C > kBwdMost ? 2 * N : 0)) * 4;
+  return (bwd_parts(N, C) * 2 * C + (C > kNormBwdMost ? 2 * N : 0)) * 4;
 }
 
 hipError_t launch_layernorm_bwd(const void* dY, const void* X, DType t, int64_t N, int64_t C, const float* gamma,
                                 const float* mean, const float* rstd, void* dX, float* dgamma, float* dbeta,
                                 void* workspace, hipStream_t s) {
+  const bool weights = dgamma || dbeta;
+  if (!dX && !weights) return hipSuccess;
   const int64_t parts = bwd_parts(N, C);
-  float* part = static_cast<float*>(workspace);
+  float* part = weights ? static_cast<float*>(workspace) : nullptr;
+  float* stats = C > kNormBwdMost ? static_cast<float*>(workspace) + parts * 2 * C : nullptr;
   if (N > 0) {
-    const hipError_t e = t == DType::F32 ? bwd_typed<float>(dY, X, N, C, gamma, mean, rstd, dX, part, parts, s)
-                                         : bwd_typed<bf16_t>(dY, X, N, C, gamma, mean, rstd, dX, part, parts, s);
+    const hipError_t e = t == DType::F32 ? bwd_typed<float>(dY, X, N, C, gamma, mean, rstd, dX, part, stats, parts, s)
+                                         : bwd_typed<bf16_t>(dY, X, N, C, gamma, mean, rstd, dX, part, stats, parts, s);
     if (e != hipSuccess) return e;
   }
-  if (!dgamma && !dbeta) return hipSuccess;
+  if (!weights) return hipSuccess;
   hipLaunchKernelGGL(norm_sums_kernel, dim3(static_cast<uint32_t>((2 * C + kSumCols - 1) / kSumCols)),
                      dim3(kSumCols * kSumGroups), 0, s, part, static_cast<int32_t>(parts), C, dgamma, dbeta);
   return hipGetLastError();

@@ -4,6 +4,7 @@ their definitions leave, where a looser bound would pass a wrong step.
 Tolerances are those of test_gpu_block.py: u = 2^-24 per term of an fp32 sum,
 half a step of the output's type for its one rounding.
 """
+import ctypes
 import math
 
 import pytest
@@ -121,6 +122,44 @@ def test_layernorm_mean_is_as_good_as_a_sum(cci, C, dt):  # noqa: F811
     want = X.double().mean(1)
     off = (mean - want).abs().mean().item()
     assert off <= U * (3.8 / C ** 0.5 + want.abs().mean().item()), off / U
+
+
+@pytest.mark.parametrize("dt", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("N,C", [(5, 40), (70, 1001), (9, 4096), (3, 16384), (3, 16392), (700, 16393)])
+def test_layernorm_bwd_in_parts(cci, N, C, dt):  # noqa: F811
+    """The gradients that are wanted are those of the whole call; without the weights' nothing is written to the
+    workspace, which need not be there for rows of up to 16384."""
+    g = gen(N + C)
+    X, dY, gamma = normal(g, N, C, dt=dt), normal(g, N, C, dt=dt), normal(g, C) + 1
+    _, mean, rstd = cci.layernorm(X, gamma)
+    whole = cci.layernorm_bwd(dY, X, mean, rstd, gamma)
+    dX, dg, db = cci.layernorm_bwd(dY, X, mean, rstd, gamma, need_dw=False)
+    assert dg is None and db is None and torch.equal(dX, whole[0])
+    dX, dg, db = cci.layernorm_bwd(dY, X, mean, rstd, gamma, need_dx=False)
+    assert dX is None and torch.equal(dg, whole[1]) and torch.equal(db, whole[2])
+    assert cci.layernorm_bwd(dY, X, mean, rstd, gamma, need_dx=False, need_dw=False) == (None, None, None)
+    nb = ctypes.c_size_t()
+    assert cci.raw().cci_layernorm_bwd_workspace(N, C, ctypes.byref(nb)) == cci.OK
+    out, ws = Guarded((N, C), dt), torch.full((nb.value,), 0x7f, dtype=torch.uint8, device=DEV)
+
+    def call(dx, dgamma, dbeta, w):
+        return cci.raw().cci_layernorm_bwd(dY.data_ptr(), X.data_ptr(), cci._code(dt), N, C, gamma.data_ptr(), mean.data_ptr(),
+                                           rstd.data_ptr(), cci._ptr(dx), cci._ptr(dgamma), cci._ptr(dbeta), cci._ptr(w),
+                                           0 if w is None else nb.value, None)
+
+    assert call(out.t, None, None, ws) == cci.OK
+    torch.cuda.synchronize()
+    assert torch.equal(out.t, whole[0])
+    sums = nb.value - (8 * N if C > 16384 else 0)  # (long rows keep two values each behind the sums)
+    assert (ws[:sums] == 0x7f).all()
+    if C <= 16384:
+        assert call(out.t, None, None, None) == cci.OK
+    else:
+        assert call(out.t, None, None, None) == cci.EINVAL
+    only = torch.empty(C, device=DEV)
+    assert call(None, None, only, ws) == cci.OK
+    assert torch.equal(only, whole[2])
+    out.check("dX")
 
 
 # -------------------------------------------------------------- activations --
