@@ -393,29 +393,33 @@ __global__ __launch_bounds__(kSumCols * kSumGroups) void norm_sums_kernel(const 
                                                                          float* __restrict__ dbeta) {
   __shared__ float red[kSumGroups][kSumCols];
   const int col = threadIdx.x % kSumCols, grp = threadIdx.x / kSumCols;
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * kSumCols + col;  // of the 2 C sums
-  float v = 0.0f;
-  if (c < 2 * C) {
-    constexpr int kAhead = 8;  // loads in flight
-    int32_t p = grp;
-    for (; p + (kAhead - 1) * kSumGroups < P; p += kAhead * kSumGroups) {
-      float q[kAhead];
+  // (in a loop: a launch has fewer than 2^32 threads)
+  for (int64_t c0 = static_cast<int64_t>(blockIdx.x) * kSumCols; c0 < 2 * C; c0 += static_cast<int64_t>(gridDim.x) * kSumCols) {
+    const int64_t c = c0 + col;  // of the 2 C sums
+    float v = 0.0f;
+    if (c < 2 * C) {
+      constexpr int kAhead = 8;  // loads in flight
+      int32_t p = grp;
+      for (; p + (kAhead - 1) * kSumGroups < P; p += kAhead * kSumGroups) {
+        float q[kAhead];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) q[i] = part[static_cast<int64_t>(p + i * kSumGroups) * 2 * C + c];
+        for (int i = 0; i < kAhead; ++i) q[i] = part[static_cast<int64_t>(p + i * kSumGroups) * 2 * C + c];
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) v += q[i];
+        for (int i = 0; i < kAhead; ++i) v += q[i];
+      }
+      for (; p < P; p += kSumGroups) v += part[static_cast<int64_t>(p) * 2 * C + c];
     }
-    for (; p < P; p += kSumGroups) v += part[static_cast<int64_t>(p) * 2 * C + c];
-  }
-  red[grp][col] = v;
-  __syncthreads();
-  if (grp != 0 || c >= 2 * C) return;
+    __syncthreads();  // the previous columns' sums are read
+    red[grp][col] = v;
+    __syncthreads();
+    if (grp != 0 || c >= 2 * C) continue;
 #pragma unroll
-  for (int i = 1; i < kSumGroups; ++i) v += red[i][col];
-  if (c < C) {
-    if (dgamma) dgamma[c] = v;
-  } else if (dbeta) {
-    dbeta[c - C] = v;
+    for (int i = 1; i < kSumGroups; ++i) v += red[i][col];
+    if (c < C) {
+      if (dgamma) dgamma[c] = v;
+    } else if (dbeta) {
+      dbeta[c - C] = v;
+    }
   }
 }
 
@@ -520,8 +524,8 @@ hipError_t launch_layernorm_bwd(const void* dY, const void* X, DType t, int64_t 
     if (e != hipSuccess) return e;
   }
   if (!weights) return hipSuccess;
-  hipLaunchKernelGGL(norm_sums_kernel, dim3(static_cast<uint32_t>((2 * C + kSumCols - 1) / kSumCols)),
-                     dim3(kSumCols * kSumGroups), 0, s, part, static_cast<int32_t>(parts), C, dgamma, dbeta);
+  const int64_t blocks = std::min<int64_t>((2 * C + kSumCols - 1) / kSumCols, int64_t(1) << 20);
+  hipLaunchKernelGGL(norm_sums_kernel, dim3(static_cast<uint32_t>(blocks)), dim3(kSumCols * kSumGroups), 0, s, part, static_cast<int32_t>(parts), C, dgamma, dbeta);
   return hipGetLastError();
 }
 

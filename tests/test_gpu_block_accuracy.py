@@ -162,6 +162,23 @@ def test_layernorm_bwd_in_parts(cci, N, C, dt):  # noqa: F811
     out.check("dX")
 
 
+def test_layernorm_bwd_of_very_long_rows(cci):  # noqa: F811
+    """Weight gradients of more columns than a launch has threads for, 16 to a column and kind."""
+    C = (1 << 27) + 5
+    g = gen(3)
+    X, dY = normal(g, 1, C, dt=BF16), normal(g, 1, C, dt=BF16)
+    mean, rstd = torch.tensor([0.25], device=DEV), torch.tensor([1.5], device=DEV)
+    dX, dg, db = cci.layernorm_bwd(dY, X, mean, rstd)
+    assert torch.equal(db, dY[0].float())
+    want = dY[0].float() * ((X[0].float() - 0.25) * 1.5)
+    assert torch.allclose(dg, want, rtol=8 * U, atol=0)  # three roundings either way
+    q, xh = dY[0].double(), (X[0].double() - 0.25) * 1.5
+    ref = 1.5 * (q - q.mean() - xh * (q * xh).mean())
+    # a thread adds 2^14 terms, then 10 levels
+    slack = 1.5 * (2 ** 14 + 10) * U * (q.abs().mean() + xh.abs() * (q * xh).abs().mean()) + 16 * U * (q.abs() + xh.abs())
+    within(dX[0], ref, HALF[BF16] * ref.abs() + slack * (1 + HALF[BF16]), "dX")
+
+
 # -------------------------------------------------------------- activations --
 
 def act_parts(x, name):
