@@ -350,7 +350,6 @@ hipError_t launch_grad_t(GParams p, hipStream_t s) {
   p.nob = (p.O + kSide - 1) / kSide;
   p.ncb = (p.C + kSide - 1) / kSide;
   const int64_t grid = static_cast<int64_t>(p.nob) * p.ncb;
-  if (grid > 0x7fffffff) return hipErrorInvalidConfiguration;
   p.grid8 = grid % kXcds == 0 ? static_cast<int32_t>(grid / kXcds) : 0;
   static std::atomic<int8_t> lds_set[kMaxDevices];
   const hipError_t attr = set_lds_limit_once(lds_set, reinterpret_cast<const void*>(&grad_mfma_kernel<T, DT>), kLds);
@@ -367,7 +366,7 @@ bool grad_mfma_supports(const void* dY, const void* X, DType t, int64_t N, int64
   const auto al = [](const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0; };
   if (!al(dY) || !al(X)) return false;
   const int64_t lim = static_cast<int64_t>(kOOB);
-  return N * O * 2 < lim && N * C * 2 < lim;
+  return N * O * 2 < lim && N * C * 2 < lim && (O + 255) / 256 * ((C + 255) / 256) <= kMostThreads / Tile<8>::kThreads;
 }
 
 hipError_t launch_grad_mfma(const void* dY, const void* X, int64_t N, int64_t C, const uint8_t* idx, int64_t O,

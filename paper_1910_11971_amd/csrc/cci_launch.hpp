@@ -35,6 +35,10 @@ inline hipError_t set_lds_limit_once(std::atomic<int8_t> (&done)[kMaxDevices], c
   return e;
 }
 
+// Threads of a launch at most.  The runtime counts them in 32 bits: more are
+// launched as what is left of the number, without an error.
+constexpr int64_t kMostThreads = 0xffffffff;
+
 enum class DType { F32 = 0, BF16 = 1 };
 
 struct ProductArgs {

@@ -93,7 +93,8 @@ struct TParams {
   const float* scale;
   const float* bias;
   uint32_t nnb, nwb;  // tile counts along TN and TW
-  uint32_t grid;
+  uint32_t grid;      // workgroups of this launch
+  uint32_t base;      // and of those before it
 };
 
 // PL: packed units per lane that are loaded a chunk ahead; 0: more, loaded
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(TEAMS * kThreads, TEAMS > 2 ? TEAMS : 2) void tile_
   // ---- tile of this workgroup: dispatch places workgroup b on XCD b % 8; L
   // numbers the workgroups of one XCD consecutively, in bands of four row
   // blocks x every weight block, so that an XCD's L2 holds few of either.
-  const uint32_t L = xcd_order(blockIdx.x, p.grid);
+  const uint32_t L = p.base + xcd_order(blockIdx.x, p.grid);
   const uint32_t per = 4u * p.nwb, band = L / per, within = L - band * per;
   const uint32_t rows = min(4u, p.nnb - 4u * band);
   const uint32_t wb = within / rows, nb = 4u * band + (within - wb * rows);
@@ -570,15 +571,19 @@ hipError_t launch(const TParams& q, hipStream_t s) {
   const int64_t along_w = MODE == kBack ? p.C : p.O;
   const int64_t nnb = (along_n + TN - 1) / TN, nwb = (along_w + TW - 1) / TW;
   if (nnb > 0x7fffffff / 8 || nwb > 0x7fffffff / 8 || nnb * nwb > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const uint32_t grid = static_cast<uint32_t>(nnb * nwb);
   p.nnb = static_cast<uint32_t>(nnb);
   p.nwb = static_cast<uint32_t>(nwb);
-  p.grid = grid;
   static std::atomic<int8_t> lds_set[kMaxDevices];
   const hipError_t e = set_lds_limit_once(lds_set, reinterpret_cast<const void*>(&tile_kernel<T, MODE, TN, TW, PL, TEAMS>), kLds);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((tile_kernel<T, MODE, TN, TW, PL, TEAMS>), dim3(grid), dim3(TEAMS * kThreads), kLds, s, p);
-  return hipGetLastError();
+  constexpr int64_t kMost = kMostThreads / (TEAMS * kThreads) / 8 * 8;  // workgroups of a launch
+  for (int64_t first = 0; first < nnb * nwb; first += kMost) {
+    p.base = static_cast<uint32_t>(first);
+    p.grid = static_cast<uint32_t>(nnb * nwb - first < kMost ? nnb * nwb - first : kMost);
+    hipLaunchKernelGGL((tile_kernel<T, MODE, TN, TW, PL, TEAMS>), dim3(p.grid), dim3(TEAMS * kThreads), kLds, s, p);
+    if (const hipError_t f = hipGetLastError(); f != hipSuccess) return f;
+  }
+  return hipSuccess;
 }
 
 template <typename T, int MODE, int TN, int TW, int TEAMS>

@@ -336,7 +336,6 @@ hipError_t launch(SParams p, hipStream_t s) {
   const int64_t along = MODE == kGated ? p.O / 2 : p.C;
   constexpr int R = MODE == kGated ? 8 * WB : 16 * WB;
   const int64_t nnb = (p.N + 16 * NT - 1) / (16 * NT), nwb = (along + R - 1) / R;
-  if (nnb * nwb > 0x7fffffff) return hipErrorInvalidConfiguration;
   const uint32_t grid = static_cast<uint32_t>(nnb * nwb);
   p.nnb = static_cast<uint32_t>(nnb);
   p.nwb = static_cast<uint32_t>(nwb);
@@ -404,6 +403,8 @@ hipError_t launch_nt(const BlockProduct& a, int wb, int rows, hipStream_t s) {
 }  // namespace
 
 bool wave_split_supports(const BlockProduct& a, bool gated, int wb) {
+  const int64_t out = gated ? a.O / 2 : a.C, width = (gated ? 8 : 16) * wb;
+  if ((a.N + 15) / 16 * ((out + width - 1) / width) > kMostThreads / kThreads) return false;
   return a.t == DType::BF16 && a.N >= 1 && units(gated, wb, a.G, a.K) <= 4 &&
          (gated ? wb >= 2 : a.C >= 16 * wb);
 }

@@ -233,3 +233,28 @@ def test_activations_far_out(cci, act):  # noqa: F811
     at0 = {"none": 1.0, "relu": 0.0}.get(act, 0.5)
     d = torch.where(g == 0, at0, ((g > 0) | none).float())
     assert torch.equal(H[0], 0.5 * a) and torch.equal(dpre[0, F:], a) and torch.equal(dpre[0, :F], 0.5 * d)
+
+
+# -------------------------------------------------- more tiles than a launch --
+
+@pytest.mark.parametrize("N,C,G", [(3, 1 << 18, 256), (33, 1 << 19, 128)])
+def test_packed_gradient_of_a_very_large_layer(cci, N, C, G):  # noqa: F811
+    """2^20 weight rows: the packed gradient has more tiles than one launch has threads for.  Samples of small whole
+    numbers: every sum is exact."""
+    F, K = 1 << 19, 1
+    g = gen(N)
+    idx = torch.randint(0, G, (2 * F // G, K, C), generator=g, device=DEV, dtype=torch.uint8)
+    X = torch.randint(-2, 3, (N, C), generator=g, device=DEV).to(BF16)
+    dH = torch.randint(-2, 3, (N, F), generator=g, device=DEV).to(BF16)
+    pre = torch.randint(-2, 3, (N, 2 * F), generator=g, device=DEV).to(BF16)
+    vals = torch.empty((2 * F // G, K, C), dtype=BF16, device=DEV)  # (not read without dX)
+    dpre, _, dv = cci.gated_spmm_bwd(dH, pre, X, vals, idx, G, act="none", need_dx=False)
+    d, x = dpre.float(), X.float()
+    assert torch.equal(d, torch.cat((dH.float() * pre[:, F:].float(), dH.float() * pre[:, :F].float()), 1))
+    groups, step = 2 * F // G, 64
+    for lo in [*range(0, groups, step * (1 if N < 8 else 8)), groups - step]:
+        rows = (torch.arange(lo, lo + step, device=DEV)[:, None] * G + idx[lo:lo + step, 0].long())
+        want = torch.zeros((step, C), device=DEV)
+        for n in range(N):
+            want += d[n][rows] * x[n]
+        assert torch.equal(dv[lo:lo + step, 0].float(), want.to(BF16).float()), lo
