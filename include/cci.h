@@ -251,9 +251,9 @@ cci_algo cci_auto_algo(cci_dtype x_t, cci_dtype val_t, int64_t N, int64_t C,
 /* The family that the calling thread's last cci_spmm / cci_conv_im2col call
  * (plain or _algo) with rows to compute launched or tried to launch:
  * CCI_ALGO_AUTO before the first.  A refused call leaves it as it was.
- * (cci_spmm_adapters makes such a call, unless the product would run on the
- * vector ALUs or be refused there: then it runs on kernels of its own and
- * leaves this as it was.) */
+ * (cci_spmm_adapters makes such a call, or runs its product on kernels of its
+ * own and leaves this as it was: in bf16 one that would run on the vector
+ * ALUs, in fp32 one that is faster so, in either one that would be refused.) */
 cci_algo cci_last_algo(void);
 
 /* ------------------------------------------------------------------------

@@ -97,17 +97,37 @@ size_t adapter_workspace(int64_t N, int64_t C, int64_t O, int64_t L, int32_t R) 
   return adapter_base_bytes(N, O) + static_cast<size_t>(part);
 }
 
+// Whether an fp32 product beside adapters runs on the tile kernels: cci_spmm
+// has the vector ALUs alone for it.  Those take up to 256 rows in one pass over
+// the packed weights, whose length (C K entries of a group, one after another)
+// and kept multiply-adds set the time; from 257 rows on they are far behind.
+// Tiles take a time per chunk of 32 columns and round of 256 tiles, whatever
+// is kept.  us of a call, vector ALUs / tiles, and what is chosen:
+//   640 -> 352, G = 8, K = 2    64 rows 14 / 28 v, 256 rows 30 / 34 v
+//   640 -> 352, G = 32, K = 8   64 rows 33 / 30 t, 256 rows 56 / 36 t
+//   256 -> 512, G = 8, K = 4    64 rows 12 / 19 v, 128 rows 22 / 25 v, 256 rows 28 / 25 t
+//   1024 -> 1024, G = 16, K = 4 64 rows 28 / 37 v, 96 rows 44 / 45 v, 128 rows 51 / 43 t
+//   1024 -> 1024, G = 16, K = 8 24 rows 28 / 37 v, 48 rows 42 / 37 t
+//   4096 -> 4096, G = 16, K = 4 16 rows 82 / 109 v, 24 rows 116 / 111 t, 64 rows 277 / 114 t
+//   320 -> 128, G = 8, K = 2    304 rows 273 / 28 t
+// On 48 drawn shapes of 1 to 468 rows the choice takes 1.01 times the better form's time.
+bool f32_on_tiles(const BlockProduct& p) {
+  if (p.G != 2 && p.G != 4 && p.G != 8 && p.G != 16 && p.G != 32) return true;  // cci_spmm refuses them
+  if (p.N > 256) return true;
+  const double kept = static_cast<double>(p.N) * static_cast<double>(p.O) * static_cast<double>(p.C) * p.K / p.G;
+  const double walk = static_cast<double>(p.C) * p.K * (p.G <= 16 ? 2.3e-3 : 4.1e-3);
+  const double chunks = static_cast<double>((p.C + 31) / 32);
+  const double filled = std::max(1.0, static_cast<double>(p.N) * static_cast<double>(p.O) / (256.0 * 64 * 64));
+  return 3.0 + 0.9 * chunks * filled < walk + kept * (p.K == 1 ? 1.8e-6 : 0.85e-6);
+}
+
 // cci_spmm runs a product on kernels made for its shape, except in bf16 what
 // it leaves to the vector ALUs, at 1/32 of the matrix cores' rate (239 x 3896
 // -> 416, G = 32, K = 8: 271 us there, 28 here), and groups that it refuses.
 // Rows that are not a multiple of 8 elements long have a form there that reads
 // element by element.
-// In fp32 it has the vector ALUs alone, which are ahead for few rows; with the
-// adapters' own kernels, tiles / that product alone: 8 rows 640 -> 352 24 / 10,
-// 4096 -> 4096 (G = 16, K = 4) 106 / 44; 64 rows 26 / 11 and 109 / 293; 429
-// rows 30 / 393 and 209 / 2714; 2000 rows 2048 -> 2048, G = 32, K = 1, 201 / 799.
 bool tile_product(const BlockProduct& p) {
-  if (p.t == DType::F32) return p.N > 32 || (p.G != 2 && p.G != 4 && p.G != 8 && p.G != 16 && p.G != 32);
+  if (p.t == DType::F32) return f32_on_tiles(p);
   if (p.C % 8 != 0 || p.O % 8 != 0) return true;
   ProductArgs a{};
   a.X = p.X;
