@@ -24,8 +24,8 @@
 // Fragments read from rows of memory cost the L1 one access per lane and 16
 // bytes; that and the latency of a chain of loads bind.  3001 rows, C = O =
 // 4096, R = 32, runs of 377 rows: shrink 13.9 us (18.8 with tiles of 16 rows),
-// expand 27.7, which reads 49 MB of P and writes 24.6 of D; 32 rows of 16 adapters, R = 16: 4.6
-// and 5.4, two launches' own time for the most part.
+// expand 28, which reads 49 MB of P and writes 24.6 of D; 32 rows of 16 adapters, R = 16: 4.2
+// and 5.3, two launches' own time for the most part.
 #include <algorithm>
 #include <type_traits>
 

@@ -44,12 +44,12 @@ inline int64_t groups_in(int64_t span, int64_t G) {
   return span % G == 0 ? span / G : G % span == 0 ? 1 : (span - 2) / G + 2;
 }
 
-// bf16 gated products and input gradients over few tiles of up to 64 rows x
-// 16 wb weight rows (wb 4, 2; input gradients also 1): 8 wb outputs (gated) or
-// 16 wb columns.
 // cci_spmm would run this product on the sparse-MAC kernels, or refuse it (cci_api.cpp).
 bool spmm_without_matrix_cores(ProductArgs a);
 
+// bf16 gated products and input gradients over few tiles of up to 64 rows x
+// 16 wb weight rows (wb 4, 2; input gradients also 1): 8 wb outputs (gated) or
+// 16 wb columns.
 bool wave_split_supports(const BlockProduct& a, bool gated, int wb);
 hipError_t launch_wave_split(const BlockProduct& a, bool gated, int wb, int rows, hipStream_t s);
 // bf16 gated products and input gradients in tiles of 32 pt rows (pt 4 or 8)

@@ -21,7 +21,7 @@
 // so its zero fill and its writes are ordered by the LDS itself.
 // The LDS binds where tiles fill the chip (zero fill, one two-byte store per
 // kept weight, fragment reads: gated 4096 x 4096 -> 8192, G = 16, K = 4: 815
-// us, 504 on the wide tiles), a memory latency per chunk where they do not
+// us, 480 on the wide tiles, both under the profiler), a memory latency per chunk where they do not
 // (back, 777 x 5456 -> 1000: 166 us with one team of waves, 65 with four; 1424
 // x 3584 -> 160: 23, and 39 before its loads at the last columns were whole).
 #include "cci_act.hpp"

@@ -3,6 +3,7 @@ choice, with stand-ins for the HIP runtime)."""
 import os
 import random
 import runpy
+import shutil
 
 import pytest
 
@@ -15,6 +16,8 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 @pytest.fixture(scope="module")
 def launched(tmp_path_factory):
+    if shutil.which("g++") is None:
+        pytest.skip("needs g++")
     tmp = str(tmp_path_factory.mktemp("log"))
     return lambda calls: kernels(calls, tmp)
 
